@@ -334,6 +334,72 @@ cdq_status cdq_layer_loss_static(const float* H, const void* W, cdq_dtype wt, lo
                                  const float* scale, const float* zero, const unsigned char* Q,
                                  double* loss, double* per_col, void* stream);
 
+/*
+ * ---- A solved layer at work -------------------------------------------------------------------------------------------------
+ * The paper ends with codes, scales and zeros; a model is run, evaluated and tuned with W_hat = a * Q + b in the place of W (paper: Section 3
+ * "Notation"; the weights stay quantized, the activations are 16 bits: "w3a16").  The calls below take a layer in that form.
+ */
+
+/* Activation after the product: z, max(z, 0), z / (1 + e^-z), z Phi(z), and Phi's form by tanh. */
+typedef enum { CDQ_ACT_NONE = 0, CDQ_ACT_RELU = 1, CDQ_ACT_SILU = 2, CDQ_ACT_GELU = 3, CDQ_ACT_GELU_TANH = 4 } cdq_act;
+
+/* A layer with packed codes.  All pointers are device pointers owned by the caller; the struct itself lives on the host and is read during the call. */
+typedef struct {
+  const void* codes;   /* from cdq_pack, cdq_packed_bytes(bits, d_in, d_out) bytes, 16-byte aligned */
+  const float* scale;  /* [d_in/g, d_out] */
+  const float* zero;   /* [d_in/g, d_out] */
+  long long d_in, d_out;
+  int bits;            /* 1..8 */
+  int group_size;      /* 0: per-channel */
+} cdq_packed_layer;
+
+/*
+ * Codes [layers, d_in, d_out] (one byte each, dense) into the packed layout and back.  A code takes 2, 3, 4 or 8 bits (5 to 8 bits take 8), in
+ * blocks of 128 inputs x 16 columns; sizes that are not multiples are padded.  `layers` layers of one shape lie one after the other, cdq_packed_bytes
+ * apart (the experts of cdq_moe).  Codes above 2^bits - 1 lose their upper bits.  One pass, asynchronous, no workspace.
+ * Errors: CDQ_ERR_INVALID_ARG (NULL, bits outside 1..8, codes not 16-byte aligned), CDQ_ERR_SHAPE (a size below 1), CDQ_ERR_UNSUPPORTED
+ * (d_in > 65535, d_out > 2^23, layers > 65535).
+ */
+size_t cdq_packed_bytes(int bits, long long d_in, long long d_out);   /* of one layer; 0 for bad arguments */
+cdq_status cdq_pack(const unsigned char* Q, long long layers, long long d_in, long long d_out, int bits, void* codes, void* stream);
+cdq_status cdq_unpack(const void* codes, long long layers, long long d_in, long long d_out, int bits, unsigned char* Q, void* stream);
+
+/*
+ * Y = act(X W_hat + bias) + residual, W_hat = a * Q + b of the layer (paper: Section 3 "Notation").
+ *   X         [n, d_in] of type xt, leading dimension ldx (elements).
+ *   bias      [d_out] fp32, may be NULL.
+ *   residual  [n, d_out] of type xt, leading dimension ldr, may be NULL; may be Y itself (same pointer and leading dimension).
+ *   Y         [n, d_out] of type xt, leading dimension ldy; must not overlap X.
+ *   Z         [n, d_out] of type xt, leading dimension ldz, may be NULL: the pre-activation X W_hat + bias, for cdq_linear_backward.
+ * Arithmetic: with z = 2^(bits-1) the products X_t (Q_t - z) of every group t run on bf16 tensor cores whose operands are exact (fp32 X: as the sum of
+ * three bf16 terms) with fp32 sums; scales and zeros meet the sums in fp32; one rounding at the end.  Groups that are not multiples of 32 run
+ * on the fp32 units.  The order of the sums is fixed by the sizes: equal calls give equal bits.  A row of X with an entry that is not finite
+ * gives a row that is not finite (NaN or infinite); other rows are not touched.
+ * Workspace: cdq_linear_workspace_bytes (0 up to 16 rows).  Asynchronous; nothing is kept between calls.
+ * Errors: CDQ_ERR_INVALID_ARG (NULL, bad enum, bits, misaligned codes), CDQ_ERR_SHAPE (n or a size below 1, d_in % g, a leading
+ * dimension too small), CDQ_ERR_UNSUPPORTED (d_in > 65535, d_out > 2^23, n > 4000000), CDQ_ERR_WORKSPACE, CDQ_ERR_CUDA.
+ */
+size_t cdq_linear_workspace_bytes(const cdq_packed_layer* layer, cdq_dtype xt, long long n);
+cdq_status cdq_linear(const cdq_packed_layer* layer, const void* X, cdq_dtype xt, long long n, long long ldx, const float* bias, cdq_act act,
+                      const void* residual, long long ldr, void* Y, long long ldy, void* Z, long long ldz, void* ws, size_t ws_bytes,
+                      void* stream);
+
+/*
+ * Gradients of cdq_linear's act(X W_hat + bias) for its inputs, the codes fixed (the residual's gradient is dY itself):
+ *   dZ = dY * act'(Z);  dX = dZ W_hat^T;  dscale[t, j] = sum_n dZ[n, j] (X_t Q_t)[n, j];  dzero[t, j] = sum_n dZ[n, j] sum_{i in t} X[n, i];
+ *   dbias[j] = sum_n dZ[n, j].
+ *   dY, X, Z as in cdq_linear, all of type xt.  Z may be NULL with CDQ_ACT_NONE; X may be NULL where dscale and dzero are.
+ *   dX        [n, d_in] of type xt, leading dimension lddx, may be NULL; must not overlap X, dY or Z.
+ *   dscale, dzero [d_in/g, d_out] fp32, dbias [d_out] fp32, each may be NULL (not all four outputs).
+ * Arithmetic: dscale and dzero as in cdq_linear (exact operands, dZ in fp32).  dX of bf16 rounds dZ and W_hat to bf16 for the tensor cores, of
+ * fp32 it takes both as sums of three bf16 terms.
+ * Workspace: cdq_linear_backward_workspace_bytes.  Errors as for cdq_linear.
+ */
+size_t cdq_linear_backward_workspace_bytes(const cdq_packed_layer* layer, cdq_dtype xt, long long n);
+cdq_status cdq_linear_backward(const cdq_packed_layer* layer, const void* dY, cdq_dtype xt, long long n, long long lddy, const void* X, long long ldx,
+                               const void* Z, long long ldz, cdq_act act, void* dX, long long lddx, float* dscale, float* dzero, float* dbias,
+                               void* ws, size_t ws_bytes, void* stream);
+
 /* Bytes of workspace `which` needs for these sizes (n: rows of X for the Hessian, steps per column for
  * CDQ_CALL_BCD_SOLVE, which covers either block size; otherwise not used). */
 size_t cdq_workspace_bytes(cdq_call which, long long n, long long d_in, long long d_out,

@@ -25,8 +25,11 @@ CALL_HESSIAN, CALL_INIT_RTN, CALL_CD_SOLVE, CALL_LAYER_LOSS, CALL_INIT_OWC_CD, C
 CALL_CD_SOLVE_ROWS16 = 6
 _MODES = {"fast": MODE_FAST, "verify": MODE_FP64_VERIFY, MODE_FAST: MODE_FAST, MODE_FP64_VERIFY: MODE_FP64_VERIFY}
 
+_ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+
 EXPORTS = ["cdq_hessian", "cdq_hessian_add_lambda", "cdq_init_rtn", "cdq_init_owc_cd", "cdq_cd_solve", "cdq_cd_solve_steps", "cdq_cd_solve_with_loss", "cdq_cd_solve_rows16", "cdq_bcd_solve", "cdq_layer_loss", "cdq_layer_loss_static",
-           "cdq_workspace_bytes",
+           "cdq_workspace_bytes", "cdq_packed_bytes", "cdq_pack", "cdq_unpack", "cdq_linear", "cdq_linear_workspace_bytes",
+           "cdq_linear_backward", "cdq_linear_backward_workspace_bytes",
            "cdq_last_device_status", "cdq_last_error_detail", "cdq_status_string", "cdq_version",
            "cdq_kernel_launches", "cdq_debug_expire_wait", "cdq_debug_set_device_status"]
 
@@ -46,6 +49,11 @@ class cdq_cd_stats(ctypes.Structure):
     _fields_ = [("steps", ctypes.c_ulonglong), ("committed", ctypes.c_ulonglong),
                 ("columns_converged", ctypes.c_ulonglong), ("loss_before", ctypes.c_double),
                 ("loss_after", ctypes.c_double), ("kernel_ms", ctypes.c_double)]
+
+
+class cdq_packed_layer(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("zero", ctypes.c_void_p), ("d_in", ctypes.c_longlong),
+                ("d_out", ctypes.c_longlong), ("bits", ctypes.c_int), ("group_size", ctypes.c_int)]
 
 
 class cdq_owc_cd_stats(ctypes.Structure):
@@ -112,6 +120,17 @@ def load():
     lib.cdq_layer_loss.argtypes = [vp, vp, ci, ll, ll, ll, gp, vp, vp, vp, ctypes.POINTER(ctypes.c_double), vp, ci, vp, sz, vp]
     lib.cdq_layer_loss_static.restype = ci
     lib.cdq_layer_loss_static.argtypes = [vp, vp, ci, ll, ll, ll, gp, vp, vp, vp, ctypes.POINTER(ctypes.c_double), vp, vp]
+    lp = ctypes.POINTER(cdq_packed_layer)
+    lib.cdq_packed_bytes.restype = sz
+    lib.cdq_packed_bytes.argtypes = [ci, ll, ll]
+    lib.cdq_pack.restype = lib.cdq_unpack.restype = ci
+    lib.cdq_pack.argtypes = [vp, ll, ll, ll, ci, vp, vp]
+    lib.cdq_unpack.argtypes = [vp, ll, ll, ll, ci, vp, vp]
+    lib.cdq_linear_workspace_bytes.restype = lib.cdq_linear_backward_workspace_bytes.restype = sz
+    lib.cdq_linear_workspace_bytes.argtypes = lib.cdq_linear_backward_workspace_bytes.argtypes = [lp, ci, ll]
+    lib.cdq_linear.restype = lib.cdq_linear_backward.restype = ci
+    lib.cdq_linear.argtypes = [lp, vp, ci, ll, ll, vp, ci, vp, ll, vp, ll, vp, ll, vp, sz, vp]
+    lib.cdq_linear_backward.argtypes = [lp, vp, ci, ll, ll, vp, ll, vp, ll, ci, vp, ll, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -348,6 +367,153 @@ def cdq_layer_loss(H: torch.Tensor, W: torch.Tensor, grid: Grid, scale: torch.Te
                                pc.data_ptr() if pc is not None else None, _MODES[mode], wptr, wbytes, _stream())
     _check(st, "cdq_layer_loss")
     return (loss.value, pc) if per_col else loss.value
+
+
+# ---- solved layers at work ------------------------------------------------------------------------------------------------
+
+class PackedLayer:
+    """A layer as cdq_linear and cdq_moe take it: codes packed by cdq_pack, scale and zero [d_in/g, d_out] fp32.  Of `experts` layers of one shape
+    (cdq_moe) all three have a leading dimension.  scale and zero are the tensors that were given: updating them in place updates the layer."""
+
+    __slots__ = ("codes", "scale", "zero", "bits", "group_size", "d_in", "d_out", "experts", "device", "index", "ref")
+
+    def __init__(self, codes, scale, zero, bits, group_size, d_in, d_out, experts=0):
+        g = group_size or d_in
+        if not 1 <= bits <= 8 or group_size < 0 or d_in < 1 or d_out < 1 or d_in % g:
+            raise ValueError(f"no such layer: {bits} bits, {d_in} x {d_out} in groups of {group_size}")
+        lead = (experts,) if experts else ()
+        _need_cuda(codes, scale, zero)
+        for t, name in ((scale, "scale"), (zero, "zero")):
+            if t.dtype != torch.float32 or tuple(t.shape) != (*lead, d_in // g, d_out) or not t.is_contiguous() or t.device != codes.device:
+                raise ValueError(f"{name} has to be a contiguous fp32 tensor of shape {(*lead, d_in // g, d_out)} on {codes.device}")
+        nbytes = int(load().cdq_packed_bytes(bits, d_in, d_out)) * max(experts, 1)
+        if codes.dtype != torch.uint8 or codes.numel() != nbytes or not codes.is_contiguous():
+            raise ValueError(f"codes have to be {nbytes} packed bytes")
+        self.codes, self.scale, self.zero, self.bits, self.group_size = codes, scale, zero, bits, group_size
+        self.d_in, self.d_out, self.experts, self.device, self.index = d_in, d_out, experts, codes.device, codes.device.index
+        self.ref = ctypes.pointer(cdq_packed_layer(codes.data_ptr(), scale.data_ptr(), zero.data_ptr(), d_in, d_out, bits, group_size))
+
+
+def _call(fn, where: str, index: int, args):
+    """fn(*args, stream) on GPU `index` and its current stream."""
+    if torch.cuda.current_device() == index:
+        status = fn(*args, torch.cuda.current_stream(index).cuda_stream)
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, torch.cuda.current_stream(index).cuda_stream)
+    if status:
+        _check(status, where)
+
+
+def _rows_of(t: torch.Tensor, name: str, n: int | None, d: int, like: torch.Tensor) -> int:
+    """Checks a matrix of activations and returns its leading dimension."""
+    if t.dim() != 2 or t.shape[1] != d or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}: [{'rows' if n is None else n}, {d}] is needed")
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name} is {t.dtype} on {t.device}: {like.dtype} on {like.device} is needed")
+    if t.stride(1) != 1 and d > 1:
+        raise ValueError(f"{name} needs entries of a row side by side")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), d)
+
+
+def _scratch(nbytes: int, device, ws: "Workspace | None"):
+    """(tensor that keeps the scratch alive during the call, pointer, bytes).  Without a Workspace the scratch comes from torch's allocator for this one
+    call, so that calls on several streams, or captured into several graphs, never share one."""
+    if nbytes == 0:
+        return None, None, 0
+    if ws is not None:
+        p, b = ws.get(nbytes, device)
+        return ws.buf, p, b
+    buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return buf, buf.data_ptr(), nbytes
+
+
+def cdq_pack(Q: torch.Tensor, grid: Grid, scale: torch.Tensor, zero: torch.Tensor) -> PackedLayer:
+    """Codes [d_in, d_out] (or [experts, d_in, d_out]) u8 of a solved layer into the packed layout; scale and zero are kept as they are."""
+    _need_cuda(Q, scale, zero)
+    if Q.dtype != torch.uint8 or Q.dim() not in (2, 3) or not Q.is_contiguous() or 0 in Q.shape:
+        raise ValueError("codes have to be a contiguous u8 tensor [d_in, d_out] or [experts, d_in, d_out]")
+    d_in, d_out = Q.shape[-2:]
+    experts = Q.shape[0] if Q.dim() == 3 else 0
+    nbytes = int(load().cdq_packed_bytes(grid.bits, d_in, d_out)) * max(experts, 1)
+    codes = torch.empty(nbytes, dtype=torch.uint8, device=Q.device)
+    layer = PackedLayer(codes, scale, zero, grid.bits, grid.group_size, d_in, d_out, experts)
+    _call(load().cdq_pack, "cdq_pack", layer.index, (Q.data_ptr(), max(experts, 1), d_in, d_out, grid.bits, codes.data_ptr()))
+    return layer
+
+
+def cdq_unpack(layer: PackedLayer) -> torch.Tensor:
+    """The codes of a packed layer, one byte each."""
+    shape = (layer.experts, layer.d_in, layer.d_out) if layer.experts else (layer.d_in, layer.d_out)
+    Q = torch.empty(shape, dtype=torch.uint8, device=layer.device)
+    _call(load().cdq_unpack, "cdq_unpack", layer.index,
+          (layer.codes.data_ptr(), max(layer.experts, 1), layer.d_in, layer.d_out, layer.bits, Q.data_ptr()))
+    return Q
+
+
+def cdq_linear(X: torch.Tensor, layer: PackedLayer, bias: torch.Tensor | None = None, act: str = "none",
+               residual: torch.Tensor | None = None, out: torch.Tensor | None = None, want_z: bool = False, ws: Workspace | None = None):
+    """act(X W_hat + bias) + residual, X [n, d_in] bf16 or fp32 with any leading dimension; the result (and with want_z the pre-activation for
+    cdq_linear_backward, as (Y, Z)) is of X's type.  act: none, relu, silu, gelu, gelu_tanh.  out may be the residual itself."""
+    if layer.experts:
+        raise ValueError("a stack of experts is for cdq_moe")
+    if X.device != layer.device:
+        raise ValueError(f"X is on {X.device}, the layer on {layer.device}")
+    xt = _dtype_code(X)
+    ldx = _rows_of(X, "X", None, layer.d_in, X)
+    n, d_out = X.shape[0], layer.d_out
+    if act not in _ACTS:
+        raise ValueError(f"act is one of {', '.join(_ACTS)}")
+    if bias is not None and (bias.dtype != torch.float32 or bias.numel() != d_out or not bias.is_contiguous() or bias.device != X.device):
+        raise ValueError(f"bias has to be a contiguous fp32 tensor of {d_out} on {X.device}")
+    ldr = _rows_of(residual, "residual", n, d_out, X) if residual is not None else 0
+    if out is None:
+        Y, ldy = torch.empty((n, d_out), dtype=X.dtype, device=X.device), d_out
+    else:
+        Y, ldy = out, _rows_of(out, "out", n, d_out, X)
+    Z = torch.empty((n, d_out), dtype=X.dtype, device=X.device) if want_z else None
+    lib = load()
+    keep, wptr, wbytes = _scratch(lib.cdq_linear_workspace_bytes(layer.ref, xt, n), X.device, ws) if n > 16 or layer.group_size % 32 else (None, None, 0)
+    _call(lib.cdq_linear, "cdq_linear", layer.index,
+          (layer.ref, X.data_ptr(), xt, n, ldx, bias.data_ptr() if bias is not None else None, _ACTS[act],
+           residual.data_ptr() if residual is not None else None, ldr, Y.data_ptr(), ldy, Z.data_ptr() if Z is not None else None, d_out,
+           wptr, wbytes))
+    return (Y, Z) if want_z else Y
+
+
+def cdq_linear_backward(dY: torch.Tensor, layer: PackedLayer, X: torch.Tensor | None = None, Z: torch.Tensor | None = None, act: str = "none",
+                        want_x: bool = True, want_scales: bool = True, want_bias: bool = False, ws: Workspace | None = None) -> dict:
+    """Gradients of cdq_linear with the codes fixed: {"dX" (of dY's type), "dscale", "dzero" ([d_in/g, d_out] fp32), "dbias" ([d_out] fp32)}, None where
+    not wanted.  Z: the pre-activation that cdq_linear(want_z=True) gave (act none: not needed); X is needed for the scales alone."""
+    if layer.experts:
+        raise ValueError("a stack of experts is for cdq_moe")
+    if dY.device != layer.device:
+        raise ValueError(f"dY is on {dY.device}, the layer on {layer.device}")
+    xt = _dtype_code(dY)
+    d_in, d_out = layer.d_in, layer.d_out
+    lddy = _rows_of(dY, "dY", None, d_out, dY)
+    n = dY.shape[0]
+    if act not in _ACTS:
+        raise ValueError(f"act is one of {', '.join(_ACTS)}")
+    if not (want_x or want_scales or want_bias):
+        raise ValueError("no gradient is asked for")
+    if act != "none" and Z is None:
+        raise ValueError("the pre-activation Z is needed: cdq_linear(..., want_z=True) gives it")
+    if want_scales and X is None:
+        raise ValueError("X is needed for the gradients of scale and zero")
+    ldz = _rows_of(Z, "Z", n, d_out, dY) if act != "none" else 0
+    ldx = _rows_of(X, "X", n, d_in, dY) if want_scales else 0
+    new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=dY.device)   # noqa: E731
+    dX = new((n, d_in), dY.dtype) if want_x else None
+    dscale, dzero = (new(layer.scale.shape, torch.float32), new(layer.scale.shape, torch.float32)) if want_scales else (None, None)
+    dbias = new((d_out,), torch.float32) if want_bias else None
+    lib = load()
+    keep, wptr, wbytes = _scratch(lib.cdq_linear_backward_workspace_bytes(layer.ref, xt, n), dY.device, ws)
+    ptr = lambda t: t.data_ptr() if t is not None else None   # noqa: E731
+    _call(lib.cdq_linear_backward, "cdq_linear_backward", layer.index,
+          (layer.ref, dY.data_ptr(), xt, n, lddy, ptr(X) if want_scales else None, ldx, ptr(Z) if act != "none" else None, ldz, _ACTS[act], ptr(dX), d_in,
+           ptr(dscale), ptr(dzero), ptr(dbias), wptr, wbytes))
+    return {"dX": dX, "dscale": dscale, "dzero": dzero, "dbias": dbias}
 
 
 STATIC_SCRATCH_BYTES = 20 * 1024 * 1024

@@ -10,6 +10,7 @@
 
 #include "async_copy.cuh"
 #include "common.cuh"
+#include "api_check.cuh"
 
 namespace cdq {
 
@@ -39,6 +40,21 @@ void count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 
 static char g_error_detail[256] = "";
 void set_error_detail(const char* text) { snprintf(g_error_detail, sizeof(g_error_detail), "%s", text); }
+
+void note_cuda_error(cudaError_t e, const char* what, const char* file, int line) {
+  snprintf(g_error_detail, sizeof(g_error_detail), "%s (%s) at %s:%d: %s", cudaGetErrorName(e), cudaGetErrorString(e), file, line, what);
+}
+
+// CDQ_DEBUG_SYNC=1 in the environment synchronises the device after every step, so that an
+// asynchronous kernel failure is attributed to the step that caused it.
+bool debug_sync() {
+  static int v = -1;
+  if (v < 0) {
+    const char* e = getenv("CDQ_DEBUG_SYNC");
+    v = (e && e[0] == '1') ? 1 : 0;
+  }
+  return v == 1;
+}
 
 namespace {
 
@@ -143,33 +159,6 @@ ResidualSrc codes_src(const Layer& ly, const unsigned char* Q) {
   s.use_gamma = 0; s.L = ly.L; s.g = ly.g; s.d_out = ly.d_out;
   return s;
 }
-
-void note_cuda_error(cudaError_t e, const char* what, int line) {
-  snprintf(g_error_detail, sizeof(g_error_detail), "%s (%s) at api.cu:%d: %s", cudaGetErrorName(e),
-           cudaGetErrorString(e), line, what);
-}
-
-// CDQ_DEBUG_SYNC=1 in the environment synchronises the device after every step, so that an
-// asynchronous kernel failure is attributed to the step that caused it.
-
-bool debug_sync() {
-  static int v = -1;
-  if (v < 0) {
-    const char* e = getenv("CDQ_DEBUG_SYNC");
-    v = (e && e[0] == '1') ? 1 : 0;
-  }
-  return v == 1;
-}
-
-#define CDQ_CUDA(expr)                                  \
-  do {                                                  \
-    cudaError_t _e = (expr);                            \
-    if (_e == cudaSuccess && debug_sync()) _e = cudaDeviceSynchronize(); \
-    if (_e != cudaSuccess) {                            \
-      note_cuda_error(_e, #expr, __LINE__);             \
-      return CDQ_ERR_CUDA;                              \
-    }                                                   \
-  } while (0)
 
 // Two events per device, made on first use and kept: cdq_cd_solve times its descent kernel with them.
 cudaError_t timing_events(cudaEvent_t* ev0, cudaEvent_t* ev1) {

@@ -1,0 +1,30 @@
+// Launchers of the product of a quantized layer and its gradients (linear_*.cu), for linear_api.cu.
+#pragma once
+
+#include "packed.cuh"
+
+namespace cdq {
+
+// pack.cu
+cudaError_t launch_pack(const unsigned char* Q, long long layers, long long d_in, long long d_out, int bits, void* packed, cudaStream_t st);
+cudaError_t launch_unpack(const void* packed, long long layers, long long d_in, long long d_out, int bits, unsigned char* Q, cudaStream_t st);
+
+// What the gradients are formed from.  Z: the pre-activations (NULL: the gradient arrives at the pre-activation itself).
+struct GradIn {
+  const void* dY; const void* X; const void* Z;
+  long long lddy, ldx, ldz, n;
+  cdq_dtype xt;
+  int act;
+};
+
+// linear_simple.cu: every group size
+cudaError_t launch_linear_simple(const PackedView& w, int cw, const void* X, cdq_dtype xt, long long n, long long ldx, const Epilogue& ep, cudaStream_t st);
+cudaError_t launch_dx_simple(const PackedView& w, int cw, const GradIn& in, void* dX, long long lddx, cudaStream_t st);
+cudaError_t launch_scale_grad_simple(const PackedView& w, int cw, const GradIn& in, float* dscale, float* dzero, cudaStream_t st);
+cudaError_t launch_bias_grad(const GradIn& in, long long d_out, float* dbias, cudaStream_t st);
+
+// linear_skinny.cu: up to 16 rows, one group or groups that are multiples of 32
+bool linear_skinny_takes(const PackedView& w, long long n);
+cudaError_t launch_linear_skinny(const PackedView& w, int cw, const void* X, long long n, long long ldx, const Epilogue& ep, cudaStream_t st);
+
+}  // namespace cdq

@@ -1,0 +1,124 @@
+// extern "C" entry points for solved layers at work (packed codes, the product, its gradients): argument checks, workspace, choice of the kernel.
+#include <stdio.h>
+#include <stdlib.h>
+#include <string.h>
+
+#include "api_check.cuh"
+#include "linear.cuh"
+
+namespace cdq {
+
+cdq_status check_packed(const cdq_packed_layer* l) {
+  if (!l || !l->codes || !l->scale || !l->zero || !aligned16(l->codes)) return CDQ_ERR_INVALID_ARG;
+  if (l->bits < 1 || l->bits > 8 || l->group_size < 0) return CDQ_ERR_INVALID_ARG;
+  if (l->d_in < 1 || l->d_out < 1 || (l->group_size > 0 && l->d_in % l->group_size)) return CDQ_ERR_SHAPE;
+  if (l->d_in > 65535 || l->d_out > (1ll << 23)) return CDQ_ERR_UNSUPPORTED;
+  return CDQ_OK;
+}
+
+PackedView view_of(const cdq_packed_layer& l) {
+  PackedView v{};
+  v.codes = (const unsigned char*)l.codes; v.scale = l.scale; v.zero = l.zero;
+  v.d_in = l.d_in; v.d_out = l.d_out;
+  v.g = (int)(l.group_size > 0 ? l.group_size : l.d_in);
+  v.ng = (int)(l.d_in / v.g);
+  v.nib = (int)packed_blocks(l.d_in); v.njt = (int)packed_tiles(l.d_out);
+  v.z = 1 << (l.bits - 1);
+  // 256 (0x4380) with eight bits, else 128 + z: a bf16 number with z in its upper mantissa bits
+  const uint32_t s = l.bits == 8 ? 0x4380u : 0x4300u + (uint32_t)v.z;
+  v.sub = s | s << 16;
+  return v;
+}
+
+namespace {
+
+bool valid_type(cdq_dtype t) { return t == CDQ_F32 || t == CDQ_BF16; }
+bool valid_act(cdq_act a) { return a >= CDQ_ACT_NONE && a <= CDQ_ACT_GELU_TANH; }
+constexpr long long kMaxRows = 4000000;
+
+cdq_status check_pack(long long layers, long long d_in, long long d_out, int bits, const void* codes) {
+  if (bits < 1 || bits > 8 || !aligned16(codes)) return CDQ_ERR_INVALID_ARG;
+  if (layers < 1 || d_in < 1 || d_out < 1) return CDQ_ERR_SHAPE;
+  if (d_in > 65535 || d_out > (1ll << 23) || layers > 65535) return CDQ_ERR_UNSUPPORTED;
+  return CDQ_OK;
+}
+
+}  // namespace
+}  // namespace cdq
+
+using namespace cdq;
+
+extern "C" {
+
+size_t cdq_packed_bytes(int bits, long long d_in, long long d_out) {
+  if (bits < 1 || bits > 8 || d_in < 1 || d_out < 1) return 0;
+  return packed_bytes_of(bits, d_in, d_out);
+}
+
+cdq_status cdq_pack(const unsigned char* Q, long long layers, long long d_in, long long d_out, int bits, void* codes, void* stream) {
+  if (!Q || !codes) return CDQ_ERR_INVALID_ARG;
+  const cdq_status s = check_pack(layers, d_in, d_out, bits, codes);
+  if (s != CDQ_OK) return s;
+  CDQ_CUDA(launch_pack(Q, layers, d_in, d_out, bits, codes, (cudaStream_t)stream));
+  return CDQ_OK;
+}
+
+cdq_status cdq_unpack(const void* codes, long long layers, long long d_in, long long d_out, int bits, unsigned char* Q, void* stream) {
+  if (!Q || !codes) return CDQ_ERR_INVALID_ARG;
+  const cdq_status s = check_pack(layers, d_in, d_out, bits, codes);
+  if (s != CDQ_OK) return s;
+  CDQ_CUDA(launch_unpack(codes, layers, d_in, d_out, bits, Q, (cudaStream_t)stream));
+  return CDQ_OK;
+}
+
+size_t cdq_linear_workspace_bytes(const cdq_packed_layer* layer, cdq_dtype xt, long long n) {
+  if (check_packed(layer) != CDQ_OK || !valid_type(xt) || n < 1) return 0;
+  return 0;
+}
+
+cdq_status cdq_linear(const cdq_packed_layer* layer, const void* X, cdq_dtype xt, long long n, long long ldx, const float* bias, cdq_act act,
+                      const void* residual, long long ldr, void* Y, long long ldy, void* Z, long long ldz, void* ws, size_t ws_bytes,
+                      void* stream) {
+  const cdq_status s = check_packed(layer);
+  if (s != CDQ_OK) return s;
+  if (!X || !Y || !valid_type(xt) || !valid_act(act)) return CDQ_ERR_INVALID_ARG;
+  if (n < 1 || ldx < layer->d_in || ldy < layer->d_out || (residual && ldr < layer->d_out) || (Z && ldz < layer->d_out)) return CDQ_ERR_SHAPE;
+  if (n > kMaxRows) return CDQ_ERR_UNSUPPORTED;
+  const PackedView w = view_of(*layer);
+  const int cw = packed_width(layer->bits);
+  Epilogue ep{};
+  ep.bias = bias; ep.residual = residual; ep.Y = Y; ep.Z = Z; ep.ldr = ldr; ep.ldy = ldy; ep.ldz = ldz; ep.act = act; ep.xt = xt;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (linear_skinny_takes(w, n)) CDQ_CUDA(launch_linear_skinny(w, cw, X, n, ldx, ep, st));
+  else CDQ_CUDA(launch_linear_simple(w, cw, X, xt, n, ldx, ep, st));
+  return CDQ_OK;
+}
+
+size_t cdq_linear_backward_workspace_bytes(const cdq_packed_layer* layer, cdq_dtype xt, long long n) {
+  if (check_packed(layer) != CDQ_OK || !valid_type(xt) || n < 1) return 0;
+  return 0;
+}
+
+cdq_status cdq_linear_backward(const cdq_packed_layer* layer, const void* dY, cdq_dtype xt, long long n, long long lddy, const void* X, long long ldx,
+                               const void* Z, long long ldz, cdq_act act, void* dX, long long lddx, float* dscale, float* dzero, float* dbias,
+                               void* ws, size_t ws_bytes, void* stream) {
+  const cdq_status s = check_packed(layer);
+  if (s != CDQ_OK) return s;
+  if (!dY || !valid_type(xt) || !valid_act(act) || (act != CDQ_ACT_NONE && !Z)) return CDQ_ERR_INVALID_ARG;
+  if ((!dX && !dscale && !dzero && !dbias) || ((dscale || dzero) && !X)) return CDQ_ERR_INVALID_ARG;
+  if (n < 1 || lddy < layer->d_out || ((dscale || dzero) && ldx < layer->d_in) || (act != CDQ_ACT_NONE && ldz < layer->d_out) ||
+      (dX && lddx < layer->d_in))
+    return CDQ_ERR_SHAPE;
+  if (n > kMaxRows) return CDQ_ERR_UNSUPPORTED;
+  const PackedView w = view_of(*layer);
+  const int cw = packed_width(layer->bits);
+  GradIn in{};
+  in.dY = dY; in.X = X; in.Z = act == CDQ_ACT_NONE ? nullptr : Z; in.lddy = lddy; in.ldx = ldx; in.ldz = ldz; in.n = n; in.xt = xt; in.act = act;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dbias) CDQ_CUDA(launch_bias_grad(in, w.d_out, dbias, st));
+  if (dscale || dzero) CDQ_CUDA(launch_scale_grad_simple(w, cw, in, dscale, dzero, st));
+  if (dX) CDQ_CUDA(launch_dx_simple(w, cw, in, dX, lddx, st));
+  return CDQ_OK;
+}
+
+}  // extern "C"

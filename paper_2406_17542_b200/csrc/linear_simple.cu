@@ -1,0 +1,183 @@
+// The product of a quantized layer and its gradients on the fp32 units, for every group size: what the matrix-instruction kernels do not
+// take (groups that are not multiples of 32).  W_hat = a Q + b is formed in fp32 (one fused multiply-add) and multiplied in fp32.
+// Tiles of 64 x 64 with 4 x 4 sums per thread, 32 long; bound by the fp32 units (2 shared-memory vectors per 16 multiply-adds).
+#include "packed.cuh"
+#include "linear.cuh"
+
+namespace cdq {
+namespace {
+
+// Code of (i, j) in the packed layout, one at a time.
+__device__ __forceinline__ int code_at(const unsigned char* codes, int cw, int nib, long long i, long long j) {
+  const int p0 = cw == 2 || cw == 3 ? 8 : 16, p1 = cw == 3 ? 4 : cw == 8 ? 16 : 0;
+  const unsigned char* block = codes + ((j >> 4) * nib + (i >> 7)) * (256ll * cw);
+  const int r = (int)(i & 127), c = r >> 5, q = (r >> 3) & 3, e = r & 7, p = 4 * c + (e >> 1), half = 16 * (e & 1), at = q * 16 + (int)(j & 15);
+  auto word = [&](int v) {
+    return v < p0 / 4 ? *reinterpret_cast<const uint32_t*>(block + at * p0 + 4 * v)
+                      : *reinterpret_cast<const uint32_t*>(block + 64 * p0 + at * p1 + 4 * (v - p0 / 4));
+  };
+  if (cw == 2) return (word(p >> 3) >> (2 * (p & 7) + half)) & 3;
+  if (cw == 4) return (word(p >> 2) >> (4 * (p & 3) + half)) & 15;
+  if (cw == 8) return (word(p >> 1) >> (8 * (p & 1) + half)) & 255;
+  if (p < 15) return (word(p / 5) >> (3 * (p % 5) + half)) & 7;
+  return ((word(0) >> (15 + half)) & 1) | ((word(1) >> (15 + half)) & 1) << 1 | ((word(2) >> (15 + half)) & 1) << 2;
+}
+
+constexpr int T = 64, TK = 32;
+
+// DX: out[n, i] = sum_j dZ[n, j] W_hat[i, j]; otherwise z[n, j] = sum_i X[n, i] W_hat[i, j].
+template <bool DX>
+__global__ void __launch_bounds__(256) linear_simple_kernel(PackedView w, int cw, const void* __restrict__ X, cdq_dtype xt, long long n, long long ldx,
+                                                            const void* __restrict__ Zin, long long ldz, int act, Epilogue ep, void* dX, long long lddx) {
+  __shared__ float xs[TK][T + 4], ws[TK][T + 4];
+  const long long n0 = (long long)blockIdx.y * T, o0 = (long long)blockIdx.x * T;   // rows of X, outputs
+  const long long K = DX ? w.d_out : w.d_in, O = DX ? w.d_in : w.d_out;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  float acc[4][4] = {};
+  for (long long k0 = 0; k0 < K; k0 += TK) {
+    for (int v = threadIdx.x; v < T * TK; v += 256) {
+      const int k = v & (TK - 1), r = v / TK;
+      float x = 0.f;
+      if (n0 + r < n && k0 + k < K) {
+        x = load_x(X, xt, (n0 + r) * ldx + k0 + k);
+        if (DX && Zin) x *= act_slope(load_x(Zin, xt, (n0 + r) * ldz + k0 + k), act);
+      }
+      xs[k][r] = x;
+      const long long i = DX ? o0 + r : k0 + k, j = DX ? k0 + k : o0 + r;
+      float y = 0.f;
+      if (i < w.d_in && j < w.d_out) {
+        const long long t = i / w.g;
+        y = fmaf(w.scale[t * w.d_out + j], (float)code_at(w.codes, cw, w.nib, i, j), w.zero[t * w.d_out + j]);
+      }
+      ws[k][r] = y;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < TK; ++k) {
+      const float4 a = *reinterpret_cast<const float4*>(&xs[k][4 * ty]), b = *reinterpret_cast<const float4*>(&ws[k][4 * tx]);
+      const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[r][c] = fmaf(av[r], bv[c], acc[r][c]);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const long long tok = n0 + 4 * ty + r, o = o0 + 4 * tx + c;
+      if (tok >= n || o >= O) continue;
+      if (DX) store_y(dX, xt, tok * lddx + o, acc[r][c]);
+      else write_out(ep, tok, o, acc[r][c]);
+    }
+}
+
+// dscale[t, j] = sum_{i in t} Q_ij M_ij, dzero[t, j] = sum_{i in t} M_ij with M = X^T dZ: one block per group and 64 columns, the rows of a group
+// 64 at a time, the sums over rows and groups in a fixed order.
+__global__ void __launch_bounds__(256) scale_grad_simple_kernel(PackedView w, int cw, const void* __restrict__ X, cdq_dtype xt, long long n, long long ldx,
+                                                                const void* __restrict__ dY, long long lddy, const void* __restrict__ Zin,
+                                                                long long ldz, int act, float* dscale, float* dzero) {
+  __shared__ float xs[TK][T + 4], ds[TK][T + 4];
+  __shared__ float sums[2][16][T];
+  const long long t = blockIdx.y, j0 = (long long)blockIdx.x * T;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  float gs[4] = {}, gz[4] = {};
+  for (long long i0 = t * w.g; i0 < (t + 1) * w.g; i0 += T) {
+    const long long i1 = min(i0 + T, (t + 1) * (long long)w.g);
+    float acc[4][4] = {};
+    for (long long k0 = 0; k0 < n; k0 += TK) {
+      for (int v = threadIdx.x; v < T * TK; v += 256) {
+        const int r = v & (T - 1), k = v / T;
+        xs[k][r] = k0 + k < n && i0 + r < i1 ? load_x(X, xt, (k0 + k) * ldx + i0 + r) : 0.f;
+        float d = 0.f;
+        if (k0 + k < n && j0 + r < w.d_out) {
+          d = load_x(dY, xt, (k0 + k) * lddy + j0 + r);
+          if (Zin) d *= act_slope(load_x(Zin, xt, (k0 + k) * ldz + j0 + r), act);
+        }
+        ds[k][r] = d;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < TK; ++k) {
+        const float4 a = *reinterpret_cast<const float4*>(&xs[k][4 * ty]), b = *reinterpret_cast<const float4*>(&ds[k][4 * tx]);
+        const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[r][c] = fmaf(av[r], bv[c], acc[r][c]);
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const long long i = i0 + 4 * ty + r, j = j0 + 4 * tx + c;
+        if (i < i1 && j < w.d_out) {
+          gs[c] = fmaf((float)code_at(w.codes, cw, w.nib, i, j), acc[r][c], gs[c]);
+          gz[c] += acc[r][c];
+        }
+      }
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) { sums[0][ty][4 * tx + c] = gs[c]; sums[1][ty][4 * tx + c] = gz[c]; }
+  __syncthreads();
+  if (threadIdx.x < 2 * T) {
+    const int which = threadIdx.x / T, c = threadIdx.x % T;
+    float s = 0.f;
+    for (int r = 0; r < 16; ++r) s += sums[which][r][c];
+    float* out = which ? dzero : dscale;
+    if (out && j0 + c < w.d_out) out[t * w.d_out + j0 + c] = s;
+  }
+}
+
+// dbias[j] = sum_n dZ[n, j]: 32 columns per block, 32 rows at a time, then the 32 partial sums in ascending order.
+__global__ void __launch_bounds__(1024) bias_grad_kernel(const void* __restrict__ dY, cdq_dtype xt, long long n, long long d_out, long long lddy,
+                                                         const void* __restrict__ Zin, long long ldz, int act, float* __restrict__ dbias) {
+  __shared__ float part[32][33];
+  const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
+  const long long j = (long long)blockIdx.x * 32 + c;
+  float s = 0.f;
+  if (j < d_out)
+    for (long long k = r; k < n; k += 32) {
+      float d = load_x(dY, xt, k * lddy + j);
+      if (Zin) d *= act_slope(load_x(Zin, xt, k * ldz + j), act);
+      s += d;
+    }
+  part[r][c] = s;
+  __syncthreads();
+  if (r == 0 && j < d_out) {
+    float t = 0.f;
+    for (int v = 0; v < 32; ++v) t += part[v][c];
+    dbias[j] = t;
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_linear_simple(const PackedView& w, int cw, const void* X, cdq_dtype xt, long long n, long long ldx, const Epilogue& ep, cudaStream_t st) {
+  const dim3 grid((unsigned)((w.d_out + T - 1) / T), (unsigned)((n + T - 1) / T));
+  { linear_simple_kernel<false><<<grid, 256, 0, st>>>(w, cw, X, xt, n, ldx, nullptr, 0, 0, ep, nullptr, 0); count_launch(); }
+  return cudaGetLastError();
+}
+
+cudaError_t launch_dx_simple(const PackedView& w, int cw, const GradIn& in, void* dX, long long lddx, cudaStream_t st) {
+  const dim3 grid((unsigned)((w.d_in + T - 1) / T), (unsigned)((in.n + T - 1) / T));
+  { linear_simple_kernel<true><<<grid, 256, 0, st>>>(w, cw, in.dY, in.xt, in.n, in.lddy, in.Z, in.ldz, in.act, Epilogue{}, dX, lddx); count_launch(); }
+  return cudaGetLastError();
+}
+
+cudaError_t launch_scale_grad_simple(const PackedView& w, int cw, const GradIn& in, float* dscale, float* dzero, cudaStream_t st) {
+  const dim3 grid((unsigned)((w.d_out + T - 1) / T), (unsigned)w.ng);
+  { scale_grad_simple_kernel<<<grid, 256, 0, st>>>(w, cw, in.X, in.xt, in.n, in.ldx, in.dY, in.lddy, in.Z, in.ldz, in.act, dscale, dzero); count_launch(); }
+  return cudaGetLastError();
+}
+
+cudaError_t launch_bias_grad(const GradIn& in, long long d_out, float* dbias, cudaStream_t st) {
+  { bias_grad_kernel<<<(unsigned)((d_out + 31) / 32), 1024, 0, st>>>(in.dY, in.xt, in.n, d_out, in.lddy, in.Z, in.ldz, in.act, dbias); count_launch(); }
+  return cudaGetLastError();
+}
+
+}  // namespace cdq

@@ -1,0 +1,122 @@
+// Codes [d_in, d_out] <-> the packed layout of packed.cuh.  Both directions are one pass over the bytes of both sides: a block of 128
+// inputs x 128 columns goes through shared memory, its rows read (or written) 16 bytes at a time, its pieces by one thread each.
+#include "packed.cuh"
+
+namespace cdq {
+namespace {
+
+constexpr int PI = 128, PJ = 128, PITCH = PJ + 4;   // rows 33 words apart: the reads down a column by 32 lanes of consecutive columns take one pass
+
+template <int CW>
+__device__ __forceinline__ void put_code(uint32_t* w, int m, uint32_t code) {
+  const int p = m >> 1, half = 16 * (m & 1);
+  if (CW == 2) w[p >> 3] |= code << (2 * (p & 7) + half);
+  else if (CW == 4) w[p >> 2] |= code << (4 * (p & 3) + half);
+  else if (CW == 8) w[p >> 1] |= code << (8 * (p & 1) + half);
+  else if (p < 15) w[p / 5] |= code << (3 * (p % 5) + half);
+  else {
+#pragma unroll
+    for (int v = 0; v < 3; ++v) w[v] |= ((code >> v) & 1u) << (15 + half);
+  }
+}
+
+template <int CW, bool VEC>
+__global__ void __launch_bounds__(256) pack_kernel(const unsigned char* __restrict__ Q, long long d_in, long long d_out, int nib, int njt,
+                                                   uint32_t mask, unsigned char* __restrict__ out) {
+  __shared__ __align__(16) unsigned char tile[PI * PITCH];
+  const int ib = blockIdx.x;
+  const long long i0 = (long long)ib * PI, j0 = (long long)blockIdx.y * PJ;
+  const long long layer = blockIdx.z;
+  Q += layer * d_in * d_out;
+  out += layer * (long long)nib * njt * Piece<CW>::BLOCK;
+  if (VEC) {
+    for (int v = threadIdx.x; v < PI * PJ / 16; v += 256) {
+      const int r = v / (PJ / 16), c = v % (PJ / 16) * 16;
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (i0 + r < d_in && j0 + c < d_out) x = *reinterpret_cast<const uint4*>(Q + (i0 + r) * d_out + j0 + c);   // d_out is a multiple of 16
+      uint32_t* t = reinterpret_cast<uint32_t*>(tile + r * PITCH + c);
+      t[0] = x.x; t[1] = x.y; t[2] = x.z; t[3] = x.w;
+    }
+  } else {
+    for (int v = threadIdx.x; v < PI * PJ; v += 256) {
+      const int r = v / PJ, c = v % PJ;
+      tile[r * PITCH + c] = i0 + r < d_in && j0 + c < d_out ? Q[(i0 + r) * d_out + j0 + c] : 0;
+    }
+  }
+  __syncthreads();
+  for (int v = threadIdx.x; v < PJ * 4; v += 256) {
+    const int q = v / PJ, c = v % PJ, jt = (int)(j0 / 16) + c / 16, row = c % 16;
+    if (jt >= njt) continue;
+    uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int m = 0; m < 32; ++m) put_code<CW>(w, m, tile[(32 * (m >> 3) + 8 * q + (m & 7)) * PITCH + c] & mask);
+    unsigned char* block = out + ((long long)jt * nib + ib) * Piece<CW>::BLOCK;
+    unsigned char* a = block + (q * 16 + row) * Piece<CW>::P0;
+    unsigned char* b = block + 64 * Piece<CW>::P0 + (q * 16 + row) * Piece<CW>::P1;
+    if (Piece<CW>::P0 == 16) *reinterpret_cast<uint4*>(a) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(a) = make_uint2(w[0], w[1]);
+    if (CW == 3) *reinterpret_cast<uint32_t*>(b) = w[2];
+    if (CW == 8) *reinterpret_cast<uint4*>(b) = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+
+template <int CW>
+__global__ void __launch_bounds__(256) unpack_kernel(const unsigned char* __restrict__ in, long long d_in, long long d_out, int nib, int njt,
+                                                     unsigned char* __restrict__ Q) {
+  __shared__ __align__(16) unsigned char tile[PI * PITCH];
+  const int ib = blockIdx.x;
+  const long long i0 = (long long)ib * PI, j0 = (long long)blockIdx.y * PJ;
+  const long long layer = blockIdx.z;
+  Q += layer * d_in * d_out;
+  in += layer * (long long)nib * njt * Piece<CW>::BLOCK;
+  for (int v = threadIdx.x; v < PJ * 4; v += 256) {
+    const int q = v / PJ, c = v % PJ, jt = (int)(j0 / 16) + c / 16, row = c % 16;
+    if (jt >= njt) continue;
+    uint32_t w[8];
+    load_piece<CW>(in + ((long long)jt * nib + ib) * Piece<CW>::BLOCK, q, row, w);
+#pragma unroll
+    for (int p = 0; p < 16; ++p) {
+      const uint32_t v2 = code_pair<CW>(w, p);
+      const int i = 32 * (p >> 2) + 8 * q + 2 * (p & 3);
+      tile[i * PITCH + c] = (unsigned char)(v2 & 0xff);
+      tile[(i + 1) * PITCH + c] = (unsigned char)(v2 >> 16);
+    }
+  }
+  __syncthreads();
+  for (int v = threadIdx.x; v < PI * PJ; v += 256) {
+    const int r = v / PJ, c = v % PJ;
+    if (i0 + r < d_in && j0 + c < d_out) Q[(i0 + r) * d_out + j0 + c] = tile[r * PITCH + c];
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_pack(const unsigned char* Q, long long layers, long long d_in, long long d_out, int bits, void* packed, cudaStream_t st) {
+  const int nib = (int)packed_blocks(d_in), njt = (int)packed_tiles(d_out);
+  const dim3 grid((unsigned)nib, (unsigned)((d_out + PJ - 1) / PJ), (unsigned)layers);
+  const uint32_t mask = (1u << bits) - 1;
+  const bool vec = d_out % 16 == 0 && aligned16(Q);
+  auto run = [&](auto kern) { kern<<<grid, 256, 0, st>>>(Q, d_in, d_out, nib, njt, mask, (unsigned char*)packed); count_launch(); };
+  switch (packed_width(bits)) {
+    case 2: vec ? run(pack_kernel<2, true>) : run(pack_kernel<2, false>); break;
+    case 3: vec ? run(pack_kernel<3, true>) : run(pack_kernel<3, false>); break;
+    case 4: vec ? run(pack_kernel<4, true>) : run(pack_kernel<4, false>); break;
+    default: vec ? run(pack_kernel<8, true>) : run(pack_kernel<8, false>); break;
+  }
+  return cudaGetLastError();
+}
+
+cudaError_t launch_unpack(const void* packed, long long layers, long long d_in, long long d_out, int bits, unsigned char* Q, cudaStream_t st) {
+  const int nib = (int)packed_blocks(d_in), njt = (int)packed_tiles(d_out);
+  const dim3 grid((unsigned)nib, (unsigned)((d_out + PJ - 1) / PJ), (unsigned)layers);
+  auto run = [&](auto kern) { kern<<<grid, 256, 0, st>>>((const unsigned char*)packed, d_in, d_out, nib, njt, Q); count_launch(); };
+  switch (packed_width(bits)) {
+    case 2: run(unpack_kernel<2>); break;
+    case 3: run(unpack_kernel<3>); break;
+    case 4: run(unpack_kernel<4>); break;
+    default: run(unpack_kernel<8>); break;
+  }
+  return cudaGetLastError();
+}
+
+}  // namespace cdq
