@@ -1,4 +1,5 @@
 // extern "C" entry points for solved layers at work (packed codes, the product, its gradients): argument checks, workspace, choice of the kernel.
+#include <math.h>
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
@@ -24,9 +25,13 @@ PackedView view_of(const cdq_packed_layer& l) {
   v.ng = (int)(l.d_in / v.g);
   v.nib = (int)packed_blocks(l.d_in); v.njt = (int)packed_tiles(l.d_out);
   v.z = 1 << (l.bits - 1);
-  // 256 (0x4380) with eight bits, else 128 + z: a bf16 number with z in its upper mantissa bits
-  const uint32_t s = l.bits == 8 ? 0x4380u : 0x4300u + (uint32_t)v.z;
-  v.sub = s | s << 16;
+  const int cw = packed_width(l.bits);
+  for (int k = 0; k < 3; ++k) {   // places 0, CW and 2 CW within the seven bits; eight bits: -256
+    const float m = l.bits == 8 ? -256.f : -(ldexpf(128.f, -k * cw) + (float)v.z);
+    uint32_t b;
+    memcpy(&b, &m, 4);
+    v.minus[k] = (b >> 16) | (b & 0xffff0000u);
+  }
   return v;
 }
 

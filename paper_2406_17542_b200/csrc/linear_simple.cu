@@ -11,7 +11,8 @@ namespace {
 __device__ __forceinline__ int code_at(const unsigned char* codes, int cw, int nib, long long i, long long j) {
   const int p0 = cw == 2 || cw == 3 ? 8 : 16, p1 = cw == 3 ? 4 : cw == 8 ? 16 : 0;
   const unsigned char* block = codes + ((j >> 4) * nib + (i >> 7)) * (256ll * cw);
-  const int r = (int)(i & 127), c = r >> 5, q = (r >> 3) & 3, e = r & 7, p = 4 * c + (e >> 1), half = 16 * (e & 1), at = q * 16 + (int)(j & 15);
+  const int r = (int)(i & 127), c = r >> 5, q = (r >> 3) & 3, e = r & 7, p = 4 * c + (e >> 1), half = 16 * (e & 1), row = (int)(j & 15);
+  const int at = 4 * row + (q ^ ((row >> (p0 == 16 ? 1 : 2)) & 3));
   auto word = [&](int v) {
     return v < p0 / 4 ? *reinterpret_cast<const uint32_t*>(block + at * p0 + 4 * v)
                       : *reinterpret_cast<const uint32_t*>(block + 64 * p0 + at * p1 + 4 * (v - p0 / 4));

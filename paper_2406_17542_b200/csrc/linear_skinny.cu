@@ -5,12 +5,16 @@
 // P_t comes from bf16 matrix instructions whose operands are exact: Q - z is an integer of at most eight bits, X is bf16 (or fp32 as three bf16 terms).
 // Scales meet the fp32 sums, once per group, so the result is that of the fp32 formula.
 //
-// Bound by the bytes of the codes.  Every warp owns tiles of 16 columns x 128 inputs (256 CW bytes in a row of DRAM, read by 8- or 16-byte loads
-// straight into the operand's registers, a few blocks ahead); WJ x WK = 8 warps of a block take WJ tiles of columns and every WK-th block of
-// inputs, and a cluster of CK thread blocks shares a long column.  The sums of warps and blocks are added in a fixed order, through shared memory
-// and the cluster's shared memory: no workspace, no atomics, one launch.
+// Bound by the bytes of the codes.  A block of WJ x WK warps takes WJ tiles of 16 columns and shares their inputs out among WK warps; a cluster of CK
+// thread blocks shares a long column.  X is staged in shared memory, the codes come by bulk copies into a ring per warp.  The sums of warps and
+// blocks are added in a fixed order, through shared memory and the cluster's shared memory: no workspace, no atomics, one launch.
 #include <cooperative_groups.h>
+#ifdef CDQ_TUNE
+#include <stdio.h>
+#include <stdlib.h>
+#endif
 
+#include "async_copy.cuh"
 #include "linear.cuh"
 #include "skinny.cuh"
 
@@ -24,110 +28,174 @@ struct Params {
   const void* X;
   long long ldx;
   Epilogue ep;
-  int n, wj, wk, ck, slab, vec;
+  int* status;
+  int n, wj_log2, wk, ck, slab, vec;
+  unsigned per_group;   // u = g / 128 (or g / 32) as floor(2^32 / u) + 1: block (or chunk) x belongs to group x * per_group >> 32 (x < 2^16); 0 for u = 1
 };
+
+constexpr unsigned kWaitCycles = 1u << 30;   // about half a second
 
 // GM: where a group can end -- 0 nowhere (one group), 1 at blocks of 128 inputs, 2 at chunks of 32.
 template <int CW, int NT, int TERMS, int GM>
-__global__ void __launch_bounds__(256) linear_skinny_kernel(const __grid_constant__ Params p) {
-  extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int W = Piece<CW>::WORDS, D = Ahead<CW>::D, BLOCK = Piece<CW>::BLOCK;
+__global__ void __launch_bounds__(256, 2) linear_skinny_kernel(const __grid_constant__ Params p) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  constexpr int W = Piece<CW>::WORDS, BLOCK = Piece<CW>::BLOCK, C = Ring<CW>::C, STAGES = Ring<CW>::STAGES, BYTES = Ring<CW>::BYTES;
   const PackedView& w = p.w;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wj = warp % p.wj, wk = warp / p.wj;
-  const int rank = (int)(blockIdx.x % p.ck), jt = (int)(blockIdx.x / p.ck) * p.wj + wj;
-  const int ib0 = (int)((long long)w.nib * rank / p.ck), ib1 = (int)((long long)w.nib * (rank + 1) / p.ck);
-  const bool on = jt < w.njt;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, WJ = 1 << p.wj_log2, wj = warp & (WJ - 1), wk = warp >> p.wj_log2;
+  const int warps = blockDim.x >> 5;
+  const int jg = p.ck == 1 ? blockIdx.x : blockIdx.x / (unsigned)p.ck, rank = blockIdx.x - jg * p.ck, jt = (jg << p.wj_log2) + wj;
+  const int ib0 = p.ck == 1 ? 0 : w.nib * rank / p.ck, ib1 = p.ck == 1 ? w.nib : w.nib * (rank + 1) / p.ck;
   const int pitch = p.slab * 128 + 32, term_at = p.n * pitch;   // rows 64 bytes apart modulo 128: eight lanes' vectors fill the banks
-  __nv_bfloat16* xs = reinterpret_cast<__nv_bfloat16*>(smem);
-  float* red = reinterpret_cast<float*>(smem + (size_t)TERMS * term_at * 2);
+  unsigned char* ring = smem + warp * (STAGES * BYTES);
+  const uint32_t bars = smem_u32(smem + warps * (STAGES * BYTES)) + warp * (STAGES * 8);
+  __nv_bfloat16* xs = reinterpret_cast<__nv_bfloat16*>(smem + warps * (STAGES * BYTES + STAGES * 8));
+  float* sums = reinterpret_cast<float*>(xs + TERMS * term_at);   // of the rows, per block (GM 2: per chunk of 32) of the slab
+  float* red = sums + p.slab * (GM == 2 ? 4 : 1) * NT * 8;
 
-  const unsigned char* tile = w.codes + (long long)(on ? jt : 0) * w.nib * BLOCK;
-  uint32_t ring[D][2 * W];
-#pragma unroll
-  for (int d = 0; d < D; ++d) {
-    const int ib = ib0 + wk + d * p.wk;
-    if (on && ib < ib1) load_block<CW>(tile + (long long)ib * BLOCK, lane, ring[d]);
+  // ---- the warp's chunks of C blocks: wk, wk + WK, ... of the blocks [ib0, ib1) ----
+  const unsigned char* tile = w.codes + (long long)jt * w.nib * BLOCK;
+  const int chunks = jt < w.njt ? (ib1 - ib0 + C - 1) / C : 0;
+  if (lane == 0) {
+    for (int s = 0; s < STAGES; ++s) mbar_init(bars + 8 * s, 1);
+    mbar_fence_init();
   }
+  __syncwarp();
+  auto request = [&](int k, int s) {   // lane 0
+    const int first = ib0 + k * C, bytes = min(C, ib1 - first) * BLOCK;
+    mbar_expect_tx(bars + 8 * s, bytes);
+    bulk_load(smem_u32(ring + s * BYTES), tile + (long long)first * BLOCK, bytes, bars + 8 * s);
+  };
+  if (lane == 0)
+    for (int s = 0; s < STAGES; ++s)
+      if (wk + s * p.wk < chunks) request(wk + s * p.wk, s);
+
   // the lane's two columns (clamped: what lies past the last column is not stored)
-  const long long j0 = min((long long)jt * 16 + (lane >> 2), w.d_out - 1), j1 = min((long long)jt * 16 + (lane >> 2) + 8, w.d_out - 1);
-  float acc[NT][4] = {}, P[NT][4] = {}, S[NT][4] = {};
+  const int row = lane >> 2, q = lane & 3;
+  const long long j0 = min((long long)jt * 16 + row, w.d_out - 1), j1 = min((long long)jt * 16 + row + 8, w.d_out - 1);
+  const float *scale0 = w.scale + j0, *zero0 = w.zero + j0;
+  const int dj = (int)(j1 - j0), part0 = Piece<CW>::part(row, q), part1 = Piece<CW>::part(row + 8, q);
+  auto scales = [&](unsigned t, float (&s)[4]) {
+    const long long at = t * w.d_out;
+    s[0] = __ldg(scale0 + at); s[1] = __ldg(zero0 + at); s[2] = __ldg(scale0 + at + dj); s[3] = __ldg(zero0 + at + dj);
+  };
+  auto group_of = [&](unsigned x) { return p.per_group ? __umulhi(x, p.per_group) : x; };
+  float sc[GM == 1 ? C : 1][4];   // scales of the next chunk's blocks
+  auto fetch_scales = [&](int k) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) scales(group_of(min(ib0 + k * C + c, w.nib - 1)), sc[GM == 1 ? c : 0]);
+  };
+  if (GM == 1 && wk < chunks) fetch_scales(wk);
+
+  float acc[NT][4] = {}, P[NT][4] = {}, S[NT][2] = {};
   int row_at[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) row_at[t] = min(t * 8 + (lane >> 2), p.n - 1) * pitch;
+  for (int t = 0; t < NT; ++t) row_at[t] = min(t * 8 + row, p.n - 1) * pitch + 8 * q;
   const float zf = (float)w.z;
-  auto scales = [&](long long i, float& a0, float& b0, float& a1, float& b1) {
-    const long long t = GM == 0 ? 0 : i / w.g;
-    a0 = __ldg(w.scale + t * w.d_out + j0); b0 = __ldg(w.zero + t * w.d_out + j0);
-    a1 = __ldg(w.scale + t * w.d_out + j1); b1 = __ldg(w.zero + t * w.d_out + j1);
-  };
-  for (int s0 = ib0; s0 < ib1; s0 += p.slab) {
+  const Codec<CW> codec(w);
+  bool ok = true;
+  int stage = 0, k = wk;
+  uint32_t phase = 0;
+  for (int s0 = ib0; s0 < ib1; s0 += p.slab) {   // a slab is a multiple of WK x C blocks, or all of them
     const int s1 = min(s0 + p.slab, ib1);
     if (s0 > ib0) __syncthreads();
-    stage_rows<TERMS>(xs, pitch, term_at, p.X, p.ldx, w.d_in, p.n, (long long)s0 * 128, (s1 - s0) * 128, p.vec);
+    stage_rows<TERMS, GM == 2 ? 32 : 128>(xs, pitch, term_at, sums, NT * 8, p.X, p.ldx, w.d_in, p.n, (long long)s0 * 128, (s1 - s0) * 128, p.vec);
     __syncthreads();
-    for (int b = s0 + wk; b < s1; b += D * p.wk) {   // a slab is a multiple of D x WK blocks: ring[d] is always the block at hand
+    for (; k < chunks && ib0 + k * C < s1; k += p.wk) {
+      ok = mbar_wait_clock32(bars + 8 * stage, phase, ok ? kWaitCycles : 1u) && ok;
+      float now[GM == 1 ? C : 1][4];
+      if (GM == 1) {
 #pragma unroll
-      for (int d = 0; d < D; ++d) {
-        const int ib = b + d * p.wk;
-        if (on && ib < s1) {
-          float a0, b0, a1, b1;
-          if (GM == 1) scales((long long)ib * 128, a0, b0, a1, b1);
-          const __nv_bfloat16* x = xs + (ib - s0) * 128 + 8 * (lane & 3);
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) now[GM == 1 ? c : 0][v] = sc[GM == 1 ? c : 0][v];
+        if (k + p.wk < chunks) fetch_scales(k + p.wk);
+      }
+      const unsigned char* codes = ring + stage * BYTES;
+      const __nv_bfloat16* x = xs + (ib0 + k * C - s0) * 128;
+      auto block = [&](int b, const float (&s1)[4]) {
+        const int at = ib0 + k * C + b - s0;   // within the slab
+        uint32_t cd[2 * W];
+        load_piece<CW>(codes + b * BLOCK, part0, cd);
+        load_piece<CW>(codes + b * BLOCK, part1, cd + W);
+        const __nv_bfloat16* xb = x + b * 128;
+        if (GM == 2) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            const long long i = (long long)ib * 128 + 32 * c;
-            if (GM == 2) {
-              if (i >= w.d_in) break;
-              scales(i, a0, b0, a1, b1);
-            }
-            mma_chunk<CW, NT, TERMS>(ring[d], c, w.sub, x + 32 * c, row_at, term_at, P, S);
-            if (GM == 2) promote<NT>(a0, b0, a1, b1, zf, P, S, acc);
+            const int chunk = (s0 + at) * 4 + c;
+            if (chunk * 32 >= (int)w.d_in) break;
+            float s[4];
+            scales(group_of(chunk), s);
+            mma_chunk<CW, NT, TERMS, true>(cd, c, codec, xb + 32 * c, row_at, term_at, P);
+            promote<NT>(s, zf, sums + (at * 4 + c) * (NT * 8) + 2 * q, P, acc);
           }
-          if (GM == 1) promote<NT>(a0, b0, a1, b1, zf, P, S, acc);
+          return;
         }
-        const int next = ib + D * p.wk;
-        if (on && next < ib1) load_block<CW>(tile + (long long)next * BLOCK, lane, ring[d]);
+        mma_chunk<CW, NT, TERMS, GM == 1>(cd, 0, codec, xb, row_at, term_at, P);
+#pragma unroll
+        for (int c = 1; c < 4; ++c) mma_chunk<CW, NT, TERMS, false>(cd, c, codec, xb + 32 * c, row_at, term_at, P);
+        const float* here = sums + at * (NT * 8) + 2 * q;
+        if (GM == 1) promote<NT>(s1, zf, here, P, acc);
+        else {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) { S[t][0] += here[8 * t]; S[t][1] += here[8 * t + 1]; }
+        }
+      };
+      if (ib0 + (k + 1) * C <= ib1) {
+#pragma unroll
+        for (int b = 0; b < C; ++b) block(b, now[GM == 1 ? b : 0]);
+      } else {
+#pragma unroll
+        for (int b = 0; b < C - 1; ++b)
+          if (ib0 + k * C + b < ib1) block(b, now[GM == 1 ? b : 0]);
       }
+      __syncwarp();
+      if (lane == 0 && k + STAGES * p.wk < chunks) request(k + STAGES * p.wk, stage);
+      if (++stage == STAGES) { stage = 0; phase ^= 1u; }
     }
   }
+  if (!ok && lane == 0) atomicCAS(p.status, (int)kFlagOk, (int)kFlagWaitTimeout);
   if (GM == 0) {
-    float a0, b0, a1, b1;
-    scales(0, a0, b0, a1, b1);
-    promote<NT>(a0, b0, a1, b1, zf, P, S, acc);
+    float s[4];
+    scales(0, s);
+    const float b0 = fmaf(zf, s[0], s[1]), b1 = fmaf(zf, s[2], s[3]);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) acc[t][v] = fmaf(v < 2 ? s[0] : s[2], P[t][v], (v < 2 ? b0 : b1) * S[t][v & 1]);
   }
   // sums of the warps that share columns, then of the cluster's blocks, both in ascending order of the inputs' share
-  const int cols = p.wj * 16, outs = cols * p.n;
+  const int cl = p.wj_log2 + 4, cols = 1 << cl, outs = cols * p.n, T = blockDim.x;
   float* mine = red + (size_t)wk * outs;
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      const int tok = t * 8 + 2 * (lane & 3) + (v & 1), col = wj * 16 + (lane >> 2) + 8 * (v >> 1);
+      const int tok = t * 8 + 2 * q + (v & 1), col = wj * 16 + row + 8 * (v >> 1);
       if (tok < p.n) mine[tok * cols + col] = acc[t][v];
     }
   __syncthreads();
-  const long long jb = (long long)(blockIdx.x / p.ck) * cols;
+  const long long jb = (long long)jg << cl;
   if (p.ck == 1) {
-    for (int o = threadIdx.x; o < outs; o += 256) {
+    for (int o = threadIdx.x; o < outs; o += T) {
       float s = red[o];
-      for (int k = 1; k < p.wk; ++k) s += red[(size_t)k * outs + o];
-      const int tok = o / cols;
-      const long long j = jb + (o - tok * cols);
+      for (int v = 1; v < p.wk; ++v) s += red[(size_t)v * outs + o];
+      const int tok = o >> cl;
+      const long long j = jb + (o & (cols - 1));
       if (j < w.d_out) write_out(p.ep, tok, j, s);
     }
   } else {
     cg::cluster_group cluster = cg::this_cluster();
-    for (int o = threadIdx.x; o < outs; o += 256) {
+    for (int o = threadIdx.x; o < outs; o += T) {
       float s = red[o];
-      for (int k = 1; k < p.wk; ++k) s += red[(size_t)k * outs + o];
+      for (int v = 1; v < p.wk; ++v) s += red[(size_t)v * outs + o];
       red[o] = s;   // read by this thread alone so far
     }
     cluster.sync();
-    for (int o = rank * 256 + threadIdx.x; o < outs; o += p.ck * 256) {
+    for (int o = rank * T + threadIdx.x; o < outs; o += p.ck * T) {
       float s = 0.f;
       for (int r = 0; r < p.ck; ++r) s += *cluster.map_shared_rank(red + o, r);
-      const int tok = o / cols;
-      const long long j = jb + (o - tok * cols);
+      const int tok = o >> cl;
+      const long long j = jb + (o & (cols - 1));
       if (j < w.d_out) write_out(p.ep, tok, j, s);
     }
     cluster.sync();   // no block's shared memory goes while another reads it
@@ -137,11 +205,19 @@ __global__ void __launch_bounds__(256) linear_skinny_kernel(const __grid_constan
 template <int CW, int NT, int TERMS, int GM>
 cudaError_t launch(const Params& p, int blocks, size_t bytes, cudaStream_t st) {
   auto kern = linear_skinny_kernel<CW, NT, TERMS, GM>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-  if (e != cudaSuccess) return e;
+  if (bytes > 48 * 1024) {   // (asked for on every call: 0.3 us of the host's time, and the attribute belongs to the current device)
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != cudaSuccess) return e;
+  }
+  const int threads = 32 * p.wk << p.wj_log2;
+  count_launch();
+  if (p.ck == 1) {
+    kern<<<blocks, threads, bytes, st>>>(p);
+    return cudaGetLastError();
+  }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)blocks);
-  cfg.blockDim = dim3(256);
+  cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = bytes;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
@@ -150,9 +226,7 @@ cudaError_t launch(const Params& p, int blocks, size_t bytes, cudaStream_t st) {
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, kern, p);
-  count_launch();
-  return e;
+  return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
 template <int CW, int NT, int TERMS>
@@ -162,7 +236,23 @@ cudaError_t launch_gm(const Params& p, int blocks, size_t bytes, cudaStream_t st
 }
 
 template <int CW>
-cudaError_t launch_cw(const Params& p, bool f32, int blocks, size_t bytes, cudaStream_t st) {
+cudaError_t run(Params& p, int wj, cudaStream_t st) {
+  const PackedView& w = p.w;
+  const bool f32 = p.ep.xt == CDQ_F32;
+  const int terms = f32 ? 3 : 1, C = Ring<CW>::C;
+  // many rows in fp32: fewer warps along the inputs, more along the columns, so that what they take in turn fits shared memory
+  while (p.wk > 1 && terms * p.n * (C * p.wk * 128 + 32) * 2 > 98304) { p.wk /= 2; wj *= 2; }
+  constexpr size_t kRing = Ring<CW>::STAGES * (Ring<CW>::BYTES + 8);
+  while ((1 << p.wj_log2) < wj) ++p.wj_log2;
+  const int units = w.g % 128 == 0 ? w.g / 128 : w.g / 32;
+  if (w.ng > 1) p.per_group = units == 1 ? 0u : (unsigned)((1ull << 32) / units + 1);
+  // inputs staged at a time: all of the block's share if they take at most 64 KB, else a multiple of what its warps take in turn
+  const int share = (w.nib + p.ck - 1) / p.ck, unit = C * p.wk;
+  const int fit = (int)((65536 / (2 * terms * p.n) - 32) / 128);
+  p.slab = share <= fit ? share : fit / unit > 0 ? fit / unit * unit : unit;
+  const size_t bytes = p.wk * wj * kRing + (size_t)terms * p.n * (p.slab * 128 + 32) * 2 + (size_t)p.wk * wj * 16 * p.n * sizeof(float) +
+                       (size_t)p.slab * (w.ng > 1 && w.g % 128 ? 4 : 1) * (p.n <= 8 ? 8 : 16) * sizeof(float);
+  const int blocks = (w.njt + wj - 1) / wj * p.ck;
   if (p.n <= 8) return f32 ? launch_gm<CW, 1, 3>(p, blocks, bytes, st) : launch_gm<CW, 1, 1>(p, blocks, bytes, st);
   return f32 ? launch_gm<CW, 2, 3>(p, blocks, bytes, st) : launch_gm<CW, 2, 1>(p, blocks, bytes, st);
 }
@@ -174,28 +264,20 @@ bool linear_skinny_takes(const PackedView& w, long long n) { return n <= 16 && (
 cudaError_t launch_linear_skinny(const PackedView& w, int cw, const void* X, long long n, long long ldx, const Epilogue& ep, cudaStream_t st) {
   Params p{};
   p.w = w; p.X = X; p.ldx = ldx; p.ep = ep; p.n = (int)n;
-  const bool f32 = ep.xt == CDQ_F32;
-  p.vec = !f32 && ldx % 8 == 0 && aligned16(X);
-  const int D = cw == 2 ? 6 : cw == 3 ? 5 : cw == 4 ? 4 : 2, terms = f32 ? 3 : 1;
-  p.wj = 2; p.wk = 4; p.ck = 1;
-  while (p.ck < 8 && (long long)((w.njt + p.wj - 1) / p.wj) * p.ck < 296 && w.nib >= 2 * p.ck * p.wk) p.ck *= 2;
+  p.vec = ep.xt == CDQ_BF16 && ldx % 8 == 0 && aligned16(X);
+  p.status = device_status_word();
+  if (!p.status) return cudaErrorInvalidSymbol;
+  int wj = 2;
+  p.wk = 4; p.ck = 1;
 #ifdef CDQ_TUNE
-  if (const char* e = getenv("CDQ_SKINNY")) sscanf(e, "%d,%d,%d", &p.wj, &p.wk, &p.ck);
+  if (const char* e = getenv("CDQ_SKINNY")) sscanf(e, "%d,%d,%d", &wj, &p.wk, &p.ck);
 #endif
-  // a slab holds at least what the rings do: many rows in fp32 take fewer warps along the inputs and more along the columns
-  while (p.wk > 1 && (long long)2 * terms * n * (D * p.wk * 128 + 32) > 163840) { p.wk /= 2; p.wj *= 2; }
-  // inputs staged at a time: all of the block's share if they take at most 64 KB, else a multiple of what the warps' rings hold
-  const int share = (w.nib + p.ck - 1) / p.ck, unit = D * p.wk;
-  const long long fit = (65536 / (2 * terms * n) - 32) / 128;
-  p.slab = share <= fit ? share : (int)(fit / unit > 0 ? fit / unit * unit : unit);
-  const size_t bytes = (size_t)terms * n * (p.slab * 128 + 32) * 2 + (size_t)p.wk * p.wj * 16 * n * sizeof(float);
-  const int blocks = (w.njt + p.wj - 1) / p.wj * p.ck;
   switch (cw) {
-    case 2: return launch_cw<2>(p, f32, blocks, bytes, st);
-    case 3: return launch_cw<3>(p, f32, blocks, bytes, st);
-    case 4: return launch_cw<4>(p, f32, blocks, bytes, st);
+    case 2: return run<2>(p, wj, st);
+    case 3: return run<3>(p, wj, st);
+    case 4: return run<4>(p, wj, st);
   }
-  return launch_cw<8>(p, f32, blocks, bytes, st);
+  return run<8>(p, wj, st);
 }
 
 }  // namespace cdq

@@ -51,8 +51,9 @@ __global__ void __launch_bounds__(256) pack_kernel(const unsigned char* __restri
 #pragma unroll
     for (int m = 0; m < 32; ++m) put_code<CW>(w, m, tile[(32 * (m >> 3) + 8 * q + (m & 7)) * PITCH + c] & mask);
     unsigned char* block = out + ((long long)jt * nib + ib) * Piece<CW>::BLOCK;
-    unsigned char* a = block + (q * 16 + row) * Piece<CW>::P0;
-    unsigned char* b = block + 64 * Piece<CW>::P0 + (q * 16 + row) * Piece<CW>::P1;
+    const int part = Piece<CW>::part(row, q);
+    unsigned char* a = block + part * Piece<CW>::P0;
+    unsigned char* b = block + 64 * Piece<CW>::P0 + part * Piece<CW>::P1;
     if (Piece<CW>::P0 == 16) *reinterpret_cast<uint4*>(a) = make_uint4(w[0], w[1], w[2], w[3]);
     else *reinterpret_cast<uint2*>(a) = make_uint2(w[0], w[1]);
     if (CW == 3) *reinterpret_cast<uint32_t*>(b) = w[2];
@@ -73,7 +74,7 @@ __global__ void __launch_bounds__(256) unpack_kernel(const unsigned char* __rest
     const int q = v / PJ, c = v % PJ, jt = (int)(j0 / 16) + c / 16, row = c % 16;
     if (jt >= njt) continue;
     uint32_t w[8];
-    load_piece<CW>(in + ((long long)jt * nib + ib) * Piece<CW>::BLOCK, q, row, w);
+    load_piece<CW>(in + ((long long)jt * nib + ib) * Piece<CW>::BLOCK, Piece<CW>::part(row, q), w);
 #pragma unroll
     for (int p = 0; p < 16; ++p) {
       const uint32_t v2 = code_pair<CW>(w, p);

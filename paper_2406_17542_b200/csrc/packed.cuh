@@ -5,8 +5,9 @@
 //   block (jt, ib) at ((jt * nib) + ib) * 256 * CW bytes, nib = ceil(d_in / 128).
 // A piece holds the 32 codes of one column whose i = 128 ib + 32 c + 8 q + e (c = 0..3, e = 0..7) share q = 0..3: what one lane of a
 // 16 x 8 x 16 matrix instruction needs of a row of its left operand, and a run of 8 inputs for every 32, so that groups that are multiples of
-// 32 end between two instructions.  A block is plane 0, [q][16 columns][P0 bytes], then plane 1, [q][16][P1]:
-// P0 = 8, 8, 16, 16 and P1 = 0, 4, 0, 16 bytes for CW = 2, 3, 4, 8.
+// 32 end between two instructions.  A block is plane 0, 64 parts of P0 bytes, then plane 1, 64 of P1: P0 = 8, 8, 16, 16 and P1 = 0, 4, 0, 16
+// bytes for CW = 2, 3, 4, 8.  Column r's quarter q is part 4 r + (q ^ (r / 2 % 4)) (r / 4 % 4 where P0 = 8): lanes that read all quarters of
+// eight columns, and lanes that read one quarter of consecutive columns, meet every bank of shared memory once.
 // Codes are stored in pairs (2p, 2p + 1), p = 4 c + e / 2 = 0..15, the first in the low half of a word and the second at the same place of the
 // high half, so that a shift and one three-input logic operation make a pair of bf16 numbers of 128 + code:
 //   CW 2: word p / 8, bit 2 (p % 8);  CW 4: word p / 4, bit 4 (p % 4);  CW 8: word p / 2, bit 8 (p % 2);
@@ -31,6 +32,7 @@ template <int CW> struct Piece {
   static constexpr int P1 = CW == 3 ? 4 : CW == 8 ? 16 : 0;
   static constexpr int WORDS = (P0 + P1) / 4;
   static constexpr int BLOCK = 256 * CW;
+  static __host__ __device__ constexpr int part(int row, int q) { return 4 * row + (q ^ ((row >> (P0 == 16 ? 1 : 2)) & 3)); }
 };
 
 // The layer as the kernels see it.
@@ -43,53 +45,89 @@ struct PackedView {
   int nib;              // blocks of 128 inputs
   int njt;              // tiles of 16 columns
   int z;                // 2^(bits - 1): the kernels multiply by code - z, an integer of at most eight bits, exact in bf16
-  uint32_t sub;         // bf16 pair of what is taken from the number that a code's bits make: 128 + z, or 256 for 8 bits (see dequant_pair)
+  uint32_t minus[3];    // bf16 pairs, see dequant_pair
 };
 
-// Makes code - z of the pair in `v` (codes in the low bits of both halves, everything else zero).  A bf16 number has seven stored
-// mantissa bits, so 0x4300 with the code in them is 128 + code, exactly.  Eight-bit codes put their top bit aside: 128 + (code & 127) minus 128 where
-// the top bit is set and 256 where it is not is code - 128 (z = 128); with fewer bits the top bit is zero and `sub` is 128 + z.
+// Codes become bf16 pairs of code - z in two or three instructions.  A bf16 number has seven stored mantissa bits, so 0x4300 with a code at bit k of
+// them is 128 + 2^k code, exactly, and a multiplication by 2^-k with an addition of -(128 2^-k + z) makes code - z, exactly: codes that lie within the
+// lowest seven bits need no shift.  (The shift and the logic operation run on the half-rate integer pipe, which bounds 2 and 3 bits: 1.25 and 1.4 of
+// its operations per pair, 1.9 and 1.8 with a shift for every code.)
+template <int CW> struct Field {
+  // pair p sits in word p / PER; its place in the word is shifted down by shift(p), which leaves it at bit at(p)
+  static constexpr int PER = CW == 2 ? 8 : CW == 3 ? 5 : CW == 4 ? 4 : 2;
+  static constexpr int BITS = CW;
+  static __host__ __device__ constexpr int place(int p) { return BITS * (p % PER); }
+  static __host__ __device__ constexpr int shift(int p) { return CW == 2 ? place(p) / 6 * 6 : CW == 3 ? place(p) / 6 * 6 : place(p); }
+  static __host__ __device__ constexpr int at(int p) { return place(p) - shift(p); }
+};
+
+// Pair p (0..15, known at compile time once the loops are unrolled) of a piece: the codes themselves.
 template <int CW>
-__device__ __forceinline__ uint32_t centre_pair(uint32_t v, uint32_t sub) {
-  uint32_t m, s = sub, r;
-  if (CW == 8) {
-    m = (v & 0x007f007fu) | 0x43004300u;
-    s = sub ^ (v & 0x00800080u);
-  } else {
-    m = v | 0x43004300u;
-  }
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(s));
+__device__ __forceinline__ uint32_t code_pair(const uint32_t* w, int p) {
+  constexpr uint32_t M = (1u << CW) - 1, MASK = M | M << 16;
+  if (CW == 3 && p == 15) return ((w[0] >> 15) & 0x00010001u) | ((w[1] >> 14) & 0x00020002u) | ((w[2] >> 13) & 0x00040004u);
+  return (w[p / Field<CW>::PER] >> Field<CW>::place(p)) & MASK;
+}
+
+__device__ __forceinline__ uint32_t bf16x2_fma(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
   return r;
 }
 
-// Pair p (0..15, known at compile time once the loops are unrolled) of a piece.
-template <int CW>
-__device__ __forceinline__ uint32_t code_pair(const uint32_t* w, int p) {
-  if (CW == 2) return (w[p >> 3] >> (2 * (p & 7))) & 0x00030003u;
-  if (CW == 4) return (w[p >> 2] >> (4 * (p & 3))) & 0x000f000fu;
-  if (CW == 8) return (w[p >> 1] >> (8 * (p & 1))) & 0x00ff00ffu;
-  if (p < 15) return (w[p / 5] >> (3 * (p % 5))) & 0x00070007u;
-  return ((w[0] >> 15) & 0x00010001u) | ((w[1] >> 14) & 0x00020002u) | ((w[2] >> 13) & 0x00040004u);
-}
-
-template <int CW>
-__device__ __forceinline__ uint32_t dequant_pair(const uint32_t* w, int p, uint32_t sub) {
-  return centre_pair<CW>(code_pair<CW>(w, p), sub);
-}
-
-// One piece: quarter q of column `row` (0..15) of a block.  The codes are read once per pass: they need no place in L1.
-template <int CW>
-__device__ __forceinline__ void load_piece(const unsigned char* block, int q, int row, uint32_t* w) {
-  const unsigned char* a = block + (q * 16 + row) * Piece<CW>::P0;
-  if (Piece<CW>::P0 == 16) {
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(a));
-  } else {
-    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(a));
+// The constants of the steps below, in registers: left to itself the compiler splits the logic operation, which can hold one constant, and loads the
+// others anew for every pair (193 instead of 115 instructions per block of 2048 codes).
+template <int CW> struct Codec {
+  static constexpr int PLACES = CW == 2 ? 3 : CW == 3 ? 2 : 1;
+  uint32_t magic, mask[PLACES], scale[PLACES], minus[PLACES];
+  __device__ __forceinline__ explicit Codec(const PackedView& w) {
+    asm volatile("mov.b32 %0, 0x43004300;" : "=r"(magic));
+#pragma unroll
+    for (int v = 0; v < PLACES; ++v) {
+      const uint32_t M = CW == 8 ? 0x7fu : ((1u << CW) - 1) << (v * CW), S = 0x3f80u - ((uint32_t)(v * CW) << 7);   // 2^-(v CW)
+      asm volatile("mov.b32 %0, %1;" : "=r"(mask[v]) : "r"(M | M << 16));
+      asm volatile("mov.b32 %0, %1;" : "=r"(scale[v]) : "r"(S | S << 16));
+      minus[v] = w.minus[v];
+    }
   }
-  const unsigned char* b = block + 64 * Piece<CW>::P0 + (q * 16 + row) * Piece<CW>::P1;
-  if (CW == 3) asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[2]) : "l"(b));
-  if (CW == 8)
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(b));
+};
+
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t set) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(set));
+  return r;
+}
+
+// code - z of pair p.  minus[v] = -(128 2^-(v CW) + z) twice; with eight bits -256, and the codes' top bits, put aside, make it -128:
+// 128 + (code & 127) - 128 where the bit is set, - 256 where it is not, is code - 128.  Five to seven bits: -(128 + z), and no top bits.
+template <int CW>
+__device__ __forceinline__ uint32_t dequant_pair(const uint32_t* w, int p, const Codec<CW>& k) {
+  if (CW == 8) {
+    const uint32_t v = w[p >> 1] >> (8 * (p & 1));
+    return bf16x2_fma(and_or(v, k.mask[0], k.magic), k.scale[0], k.minus[0] ^ (v & 0x00800080u));
+  }
+  if (CW == 3 && p == 15) return bf16x2_fma(code_pair<3>(w, 15) | k.magic, k.scale[0], k.minus[0]);
+  const int v = Field<CW>::at(p) / CW;
+  return bf16x2_fma(and_or(w[p / Field<CW>::PER] >> Field<CW>::shift(p), k.mask[v], k.magic), k.scale[v], k.minus[v]);
+}
+
+// One piece, from global or shared memory: part `part` of the block.
+template <int CW>
+__device__ __forceinline__ void load_piece(const unsigned char* block, int part, uint32_t* w) {
+  const unsigned char* a = block + part * Piece<CW>::P0;
+  const unsigned char* b = block + 64 * Piece<CW>::P0 + part * Piece<CW>::P1;
+  if (Piece<CW>::P0 == 16) {
+    const uint4 x = *reinterpret_cast<const uint4*>(a);
+    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+  } else {
+    const uint2 x = *reinterpret_cast<const uint2*>(a);
+    w[0] = x.x; w[1] = x.y;
+  }
+  if (CW == 3) w[2] = *reinterpret_cast<const uint32_t*>(b);
+  if (CW == 8) {
+    const uint4 x = *reinterpret_cast<const uint4*>(b);
+    w[4] = x.x; w[5] = x.y; w[6] = x.z; w[7] = x.w;
+  }
 }
 
 // fp32 = hi + mid + lo exactly, each a bf16 number: the upper 8, the next 8 and the last 8 bits of the mantissa, by truncation, so that nothing
