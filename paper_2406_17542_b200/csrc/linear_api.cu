@@ -40,6 +40,7 @@ namespace {
 bool valid_type(cdq_dtype t) { return t == CDQ_F32 || t == CDQ_BF16; }
 bool valid_act(cdq_act a) { return a >= CDQ_ACT_NONE && a <= CDQ_ACT_GELU_TANH; }
 constexpr long long kMaxRows = 4000000;
+bool workspace_ok(const void* ws, size_t have, size_t need) { return need == 0 || (ws && (uintptr_t)ws % kAlign == 0 && have >= need); }
 
 cdq_status check_pack(long long layers, long long d_in, long long d_out, int bits, const void* codes) {
   if (bits < 1 || bits > 8 || !aligned16(codes)) return CDQ_ERR_INVALID_ARG;
@@ -77,8 +78,9 @@ cdq_status cdq_unpack(const void* codes, long long layers, long long d_in, long 
 }
 
 size_t cdq_linear_workspace_bytes(const cdq_packed_layer* layer, cdq_dtype xt, long long n) {
-  if (check_packed(layer) != CDQ_OK || !valid_type(xt) || n < 1) return 0;
-  return 0;
+  if (check_packed(layer) != CDQ_OK || !valid_type(xt) || n < 1 || n > kMaxRows) return 0;
+  const PackedView w = view_of(*layer);
+  return linear_skinny_takes(w, n) || !linear_tc_takes(w) ? 0 : linear_tc_workspace(w, xt, n, false);
 }
 
 cdq_status cdq_linear(const cdq_packed_layer* layer, const void* X, cdq_dtype xt, long long n, long long ldx, const float* bias, cdq_act act,
@@ -94,14 +96,19 @@ cdq_status cdq_linear(const cdq_packed_layer* layer, const void* X, cdq_dtype xt
   Epilogue ep{};
   ep.bias = bias; ep.residual = residual; ep.Y = Y; ep.Z = Z; ep.ldr = ldr; ep.ldy = ldy; ep.ldz = ldz; ep.act = act; ep.xt = xt;
   cudaStream_t st = (cudaStream_t)stream;
-  if (linear_skinny_takes(w, n)) CDQ_CUDA(launch_linear_skinny(w, cw, X, n, ldx, ep, st));
-  else CDQ_CUDA(launch_linear_simple(w, cw, X, xt, n, ldx, ep, st));
+  if (linear_skinny_takes(w, n)) {
+    CDQ_CUDA(launch_linear_skinny(w, cw, X, n, ldx, ep, st));
+  } else if (linear_tc_takes(w)) {
+    if (!workspace_ok(ws, ws_bytes, linear_tc_workspace(w, xt, n, false))) return CDQ_ERR_WORKSPACE;
+    CDQ_CUDA(launch_linear_tc(w, cw, X, xt, n, ldx, ep, ws, st));
+  } else CDQ_CUDA(launch_linear_simple(w, cw, X, xt, n, ldx, ep, st));
   return CDQ_OK;
 }
 
 size_t cdq_linear_backward_workspace_bytes(const cdq_packed_layer* layer, cdq_dtype xt, long long n) {
-  if (check_packed(layer) != CDQ_OK || !valid_type(xt) || n < 1) return 0;
-  return 0;
+  if (check_packed(layer) != CDQ_OK || !valid_type(xt) || n < 1 || n > kMaxRows) return 0;
+  const PackedView w = view_of(*layer);
+  return linear_tc_takes(w) ? linear_tc_workspace(w, xt, n, true) : 0;
 }
 
 cdq_status cdq_linear_backward(const cdq_packed_layer* layer, const void* dY, cdq_dtype xt, long long n, long long lddy, const void* X, long long ldx,
@@ -120,8 +127,12 @@ cdq_status cdq_linear_backward(const cdq_packed_layer* layer, const void* dY, cd
   GradIn in{};
   in.dY = dY; in.X = X; in.Z = act == CDQ_ACT_NONE ? nullptr : Z; in.lddy = lddy; in.ldx = ldx; in.ldz = ldz; in.n = n; in.xt = xt; in.act = act;
   cudaStream_t st = (cudaStream_t)stream;
+  if (!workspace_ok(ws, ws_bytes, cdq_linear_backward_workspace_bytes(layer, xt, n))) return CDQ_ERR_WORKSPACE;
   if (dbias) CDQ_CUDA(launch_bias_grad(in, w.d_out, dbias, st));
-  if (dscale || dzero) CDQ_CUDA(launch_scale_grad_simple(w, cw, in, dscale, dzero, st));
+  if (dscale || dzero) {
+    if (linear_tc_takes(w)) CDQ_CUDA(launch_scale_grad_tc(w, cw, in, dscale, dzero, ws, st));
+    else CDQ_CUDA(launch_scale_grad_simple(w, cw, in, dscale, dzero, st));
+  }
   if (dX) CDQ_CUDA(launch_dx_simple(w, cw, in, dX, lddx, st));
   return CDQ_OK;
 }

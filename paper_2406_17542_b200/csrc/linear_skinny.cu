@@ -29,7 +29,8 @@ struct Params {
   long long ldx;
   Epilogue ep;
   int* status;
-  int n, wj_log2, wk, ck, slab, vec;
+  int n, wj_log2, wk, ck, slab, bulk;
+  int chunk;            // blocks per bulk copy, at most Ring::C: fewer where a warp has no more to do
   unsigned per_group;   // u = g / 128 (or g / 32) as floor(2^32 / u) + 1: block (or chunk) x belongs to group x * per_group >> 32 (x < 2^16); 0 for u = 1
 };
 
@@ -48,20 +49,23 @@ __global__ void __launch_bounds__(256, 2) linear_skinny_kernel(const __grid_cons
   const int pitch = p.slab * 128 + 32, term_at = p.n * pitch;   // rows 64 bytes apart modulo 128: eight lanes' vectors fill the banks
   unsigned char* ring = smem + warp * (STAGES * BYTES);
   const uint32_t bars = smem_u32(smem + warps * (STAGES * BYTES)) + warp * (STAGES * 8);
-  __nv_bfloat16* xs = reinterpret_cast<__nv_bfloat16*>(smem + warps * (STAGES * BYTES + STAGES * 8));
+  const uint32_t xbar = smem_u32(smem + warps * (STAGES * BYTES + STAGES * 8));
+  __nv_bfloat16* xs = reinterpret_cast<__nv_bfloat16*>(smem + warps * (STAGES * BYTES + STAGES * 8) + 16);
   float* sums = reinterpret_cast<float*>(xs + TERMS * term_at);   // of the rows, per block (GM 2: per chunk of 32) of the slab
   float* red = sums + p.slab * (GM == 2 ? 4 : 1) * NT * 8;
 
-  // ---- the warp's chunks of C blocks: wk, wk + WK, ... of the blocks [ib0, ib1) ----
+  // ---- the warp's chunks of blocks: wk, wk + WK, ... of the blocks [ib0, ib1) ----
+  const int cb = p.chunk;
   const unsigned char* tile = w.codes + (long long)jt * w.nib * BLOCK;
-  const int chunks = jt < w.njt ? (ib1 - ib0 + C - 1) / C : 0;
+  const int chunks = jt < w.njt ? (ib1 - ib0 + cb - 1) / cb : 0;
   if (lane == 0) {
     for (int s = 0; s < STAGES; ++s) mbar_init(bars + 8 * s, 1);
+    if (warp == 0) mbar_init(xbar, 1);
     mbar_fence_init();
   }
   __syncwarp();
   auto request = [&](int k, int s) {   // lane 0
-    const int first = ib0 + k * C, bytes = min(C, ib1 - first) * BLOCK;
+    const int first = ib0 + k * cb, bytes = min(cb, ib1 - first) * BLOCK;
     mbar_expect_tx(bars + 8 * s, bytes);
     bulk_load(smem_u32(ring + s * BYTES), tile + (long long)first * BLOCK, bytes, bars + 8 * s);
   };
@@ -82,11 +86,11 @@ __global__ void __launch_bounds__(256, 2) linear_skinny_kernel(const __grid_cons
   float sc[GM == 1 ? C : 1][4];   // scales of the next chunk's blocks
   auto fetch_scales = [&](int k) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) scales(group_of(min(ib0 + k * C + c, w.nib - 1)), sc[GM == 1 ? c : 0]);
+    for (int c = 0; c < C; ++c) if (c < cb) scales(group_of(min(ib0 + k * cb + c, w.nib - 1)), sc[GM == 1 ? c : 0]);
   };
   if (GM == 1 && wk < chunks) fetch_scales(wk);
 
-  float acc[NT][4] = {}, P[NT][4] = {}, S[NT][2] = {};
+  float acc[NT][4] = {}, P[NT][4] = {}, S[NT][4] = {};
   int row_at[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) row_at[t] = min(t * 8 + row, p.n - 1) * pitch + 8 * q;
@@ -94,13 +98,30 @@ __global__ void __launch_bounds__(256, 2) linear_skinny_kernel(const __grid_cons
   const Codec<CW> codec(w);
   bool ok = true;
   int stage = 0, k = wk;
-  uint32_t phase = 0;
-  for (int s0 = ib0; s0 < ib1; s0 += p.slab) {   // a slab is a multiple of WK x C blocks, or all of them
+  uint32_t phase = 0, xphase = 0;
+  __syncthreads();   // the barrier that all wait on is there
+  for (int s0 = ib0; s0 < ib1; s0 += p.slab) {   // a slab is a multiple of what the warps take in turn, or all of the blocks
     const int s1 = min(s0 + p.slab, ib1);
     if (s0 > ib0) __syncthreads();
-    stage_rows<TERMS, GM == 2 ? 32 : 128>(xs, pitch, term_at, sums, NT * 8, p.X, p.ldx, w.d_in, p.n, (long long)s0 * 128, (s1 - s0) * 128, p.vec);
-    __syncthreads();
-    for (; k < chunks && ib0 + k * C < s1; k += p.wk) {
+    if (TERMS == 1 && p.bulk) {   // a row per lane of the first warp; the rows' ends past d_in, if any, are filled with zeros
+      const int len = (s1 - s0) * 128, in = min(len, (int)w.d_in - s0 * 128);
+      if (warp == 0) {
+        if (lane == 0) mbar_expect_tx(xbar, p.n * in * 2);
+        __syncwarp();
+        if (lane < p.n)
+          bulk_load(smem_u32(xs + lane * pitch), (const __nv_bfloat16*)p.X + lane * p.ldx + s0 * 128, in * 2, xbar);
+      }
+      if (in < len) {
+        for (int v = threadIdx.x; v < p.n * (len - in); v += blockDim.x) xs[v / (len - in) * pitch + in + v % (len - in)] = __float2bfloat16(0.f);
+        __syncthreads();
+      }
+      ok = mbar_wait_clock32(xbar, xphase, ok ? kWaitCycles : 1u) && ok;
+      xphase ^= 1u;
+    } else {
+      stage_rows<TERMS, GM == 2 ? 32 : 128>(xs, pitch, term_at, sums, NT * 8, p.X, p.ldx, w.d_in, p.n, (long long)s0 * 128, (s1 - s0) * 128);
+      __syncthreads();
+    }
+    for (; k < chunks && ib0 + k * cb < s1; k += p.wk) {
       ok = mbar_wait_clock32(bars + 8 * stage, phase, ok ? kWaitCycles : 1u) && ok;
       float now[GM == 1 ? C : 1][4];
       if (GM == 1) {
@@ -111,9 +132,9 @@ __global__ void __launch_bounds__(256, 2) linear_skinny_kernel(const __grid_cons
         if (k + p.wk < chunks) fetch_scales(k + p.wk);
       }
       const unsigned char* codes = ring + stage * BYTES;
-      const __nv_bfloat16* x = xs + (ib0 + k * C - s0) * 128;
+      const __nv_bfloat16* x = xs + (ib0 + k * cb - s0) * 128;
       auto block = [&](int b, const float (&s1)[4]) {
-        const int at = ib0 + k * C + b - s0;   // within the slab
+        const int at = ib0 + k * cb + b - s0;   // within the slab
         uint32_t cd[2 * W];
         load_piece<CW>(codes + b * BLOCK, part0, cd);
         load_piece<CW>(codes + b * BLOCK, part1, cd + W);
@@ -125,28 +146,32 @@ __global__ void __launch_bounds__(256, 2) linear_skinny_kernel(const __grid_cons
             if (chunk * 32 >= (int)w.d_in) break;
             float s[4];
             scales(group_of(chunk), s);
-            mma_chunk<CW, NT, TERMS, true>(cd, c, codec, xb + 32 * c, row_at, term_at, P);
-            promote<NT>(s, zf, sums + (at * 4 + c) * (NT * 8) + 2 * q, P, acc);
+            mma_chunk<CW, NT, TERMS, true>(cd, c, codec, xb + 32 * c, row_at, term_at, P, S);
+            fetch_sums<NT, TERMS>(sums + (at * 4 + c) * (NT * 8) + 2 * q, S);
+            promote<NT>(s, zf, S, P, acc);
           }
           return;
         }
-        mma_chunk<CW, NT, TERMS, GM == 1>(cd, 0, codec, xb, row_at, term_at, P);
+        mma_chunk<CW, NT, TERMS, GM == 1>(cd, 0, codec, xb, row_at, term_at, P, S);
 #pragma unroll
-        for (int c = 1; c < 4; ++c) mma_chunk<CW, NT, TERMS, false>(cd, c, codec, xb + 32 * c, row_at, term_at, P);
+        for (int c = 1; c < 4; ++c) mma_chunk<CW, NT, TERMS, false>(cd, c, codec, xb + 32 * c, row_at, term_at, P, S);
         const float* here = sums + at * (NT * 8) + 2 * q;
-        if (GM == 1) promote<NT>(s1, zf, here, P, acc);
-        else {
+        if (GM == 1) {
+          fetch_sums<NT, TERMS>(here, S);
+          promote<NT>(s1, zf, S, P, acc);
+        } else if (TERMS > 1) {
 #pragma unroll
           for (int t = 0; t < NT; ++t) { S[t][0] += here[8 * t]; S[t][1] += here[8 * t + 1]; }
         }
       };
-      if (ib0 + (k + 1) * C <= ib1) {
+      const int have = min(cb, ib1 - ib0 - k * cb);
+      if (have == C) {
 #pragma unroll
         for (int b = 0; b < C; ++b) block(b, now[GM == 1 ? b : 0]);
       } else {
 #pragma unroll
         for (int b = 0; b < C - 1; ++b)
-          if (ib0 + k * C + b < ib1) block(b, now[GM == 1 ? b : 0]);
+          if (b < have) block(b, now[GM == 1 ? b : 0]);
       }
       __syncwarp();
       if (lane == 0 && k + STAGES * p.wk < chunks) request(k + STAGES * p.wk, stage);
@@ -247,10 +272,12 @@ cudaError_t run(Params& p, int wj, cudaStream_t st) {
   const int units = w.g % 128 == 0 ? w.g / 128 : w.g / 32;
   if (w.ng > 1) p.per_group = units == 1 ? 0u : (unsigned)((1ull << 32) / units + 1);
   // inputs staged at a time: all of the block's share if they take at most 64 KB, else a multiple of what its warps take in turn
-  const int share = (w.nib + p.ck - 1) / p.ck, unit = C * p.wk;
+  const int share = (w.nib + p.ck - 1) / p.ck;
+  p.chunk = (share + p.wk - 1) / p.wk < C ? (share + p.wk - 1) / p.wk : C;
+  const int unit = p.chunk * p.wk;
   const int fit = (int)((65536 / (2 * terms * p.n) - 32) / 128);
   p.slab = share <= fit ? share : fit / unit > 0 ? fit / unit * unit : unit;
-  const size_t bytes = p.wk * wj * kRing + (size_t)terms * p.n * (p.slab * 128 + 32) * 2 + (size_t)p.wk * wj * 16 * p.n * sizeof(float) +
+  const size_t bytes = p.wk * wj * kRing + 16 + (size_t)terms * p.n * (p.slab * 128 + 32) * 2 + (size_t)p.wk * wj * 16 * p.n * sizeof(float) +
                        (size_t)p.slab * (w.ng > 1 && w.g % 128 ? 4 : 1) * (p.n <= 8 ? 8 : 16) * sizeof(float);
   const int blocks = (w.njt + wj - 1) / wj * p.ck;
   if (p.n <= 8) return f32 ? launch_gm<CW, 1, 3>(p, blocks, bytes, st) : launch_gm<CW, 1, 1>(p, blocks, bytes, st);
@@ -264,7 +291,7 @@ bool linear_skinny_takes(const PackedView& w, long long n) { return n <= 16 && (
 cudaError_t launch_linear_skinny(const PackedView& w, int cw, const void* X, long long n, long long ldx, const Epilogue& ep, cudaStream_t st) {
   Params p{};
   p.w = w; p.X = X; p.ldx = ldx; p.ep = ep; p.n = (int)n;
-  p.vec = ep.xt == CDQ_BF16 && ldx % 8 == 0 && aligned16(X);
+  p.bulk = ep.xt == CDQ_BF16 && ldx % 8 == 0 && w.d_in % 8 == 0 && aligned16(X);
   p.status = device_status_word();
   if (!p.status) return cudaErrorInvalidSymbol;
   int wj = 2;

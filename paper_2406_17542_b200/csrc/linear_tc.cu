@@ -1,0 +1,606 @@
+// Y = act(X W_hat + bias) + residual, and the gradients of scales and zeros, for more rows than linear_skinny.cu takes, on the 5th-generation
+// tensor cores.
+//
+//   D_t[j, n] = sum_{i in t} (Q - z)[i, j] X[n, i]          one accumulator per group t of inputs
+//   forward   z[n, j] = sum_t a_t,j D_t[j, n] + (b_t,j + z a_t,j) S_t[n]
+//   gradients dscale[t, j] = sum_n dZ[n, j] (D_t[j, n] + z S_t[n]),   dzero[t, j] = sum_n dZ[n, j] S_t[n]
+//
+// The layer's columns are the rows of the tensor core's tile, so that a thread of the epilogue owns one column and its scale and zero are two registers.
+// Both operands are exact in bf16 (Q - z: integers of at most eight bits; X: bf16, or fp32 as three bf16 terms that share the left operand), so
+// the only roundings are those of the fp32 sums.
+//
+//   * tile 128 columns x 2 NH rows, two accumulators of NH TMEM columns; blocks of 128 inputs: X by TMA into a ring (128-byte swizzle), the codes by plain
+//     loads a few blocks ahead, made into bf16 by four warps, lane = column, and stored into TMEM, where the tensor core takes its left
+//     operand from: shared memory carries X alone;
+//   * per block the first accumulator's instructions, then the second's: while one is multiplied into, the other's group goes through the scales;
+//   * warp 0 TMA, warp 1 MMA and TMEM owner, warps 4-7 codes, warps 8-11 and 12-15 the two accumulators: acc = fma(a, D, fma(b', S, acc)) in packed fp32;
+//   * persistent blocks over the tiles; few tiles: a cluster of CK blocks shares the inputs of one and adds its sums over the cluster's shared memory.
+// A group longer than 2048 inputs is cut: the tensor core's accumulation truncates, and its error grows with the steps behind a sum.
+// Every wait is bounded, see async_copy.cuh.
+#include <cooperative_groups.h>
+#include <cuda.h>
+
+#include "async_copy.cuh"
+#include "linear.cuh"
+#include "tc5.cuh"
+
+namespace cdq {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int BJ = 128, KB = 128, FLUSH = 16;   // columns per tile, inputs per block, blocks behind one accumulator
+constexpr uint32_t SPIN = 1u << 24;
+constexpr int THREADS = 512;
+constexpr int A_COLS = KB / 2, A_STAGES = 4;    // TMEM columns of one block of codes
+constexpr int STAGE_OUT = 8 * 32 * 32 * 4;      // the epilogue's transposition, 32 x 32 per warp
+
+template <int NH, int TERMS> struct Shape {
+  static constexpr int X_BYTES = TERMS * 2 * NH * KB * 2;   // one block of X
+  static constexpr int STAGES = X_BYTES > 65536 ? 2 : X_BYTES > 49152 ? 3 : 4;
+  static constexpr size_t RAW = 1024 + (size_t)STAGES * X_BYTES + STAGE_OUT + 512;
+  static constexpr size_t SMEM = RAW < 120 * 1024 ? 120 * 1024 : RAW;   // one block per SM: it takes all of TMEM
+};
+
+struct Params {
+  PackedView w;
+  Epilogue ep;
+  GradIn in;             // gradients
+  const float* S;        // [ng, ldS] sums of the rows of X per group, zeros past n
+  float* part;           // gradients: [slots][2][ng][d_out], slot = rows / NH
+  long long n, ldS;
+  int jtiles, ttiles, ck, vec;
+  int* status;
+};
+
+// The walk over inputs that the MMA issuer and both epilogues share: segments of a block that belong to one group; `last` where the accumulator is complete.
+struct Walk {
+  int ib, ib1, k, kend, g, t, blocks;
+  bool first;
+  __device__ Walk(const PackedView& w, int a, int b)
+      : ib(a), ib1(b), k(a * KB), kend(w.ng == 1 ? w.nib * KB : (int)w.d_in), g(w.ng == 1 ? w.nib * KB : w.g), t(a * KB / g), blocks(0), first(true) {}
+  // the segment at hand: [k, seg_end)
+  __device__ int block_end() const { return min((ib + 1) * KB, kend); }
+  __device__ int seg_end() const { return min(block_end(), (t + 1) * g); }
+  __device__ bool group_ends() const { return seg_end() == (t + 1) * g; }
+  __device__ bool last() const { return group_ends() || (seg_end() == block_end() && (ib + 1 == ib1 || (blocks & (FLUSH - 1)) == FLUSH - 1)); }
+  __device__ bool done() const { return ib >= ib1; }
+  // returns true when the block is through
+  __device__ bool next() {
+    const int e = seg_end();
+    const bool b = e == block_end();
+    first = last();
+    if (e == (t + 1) * g) ++t;
+    k = e;
+    if (b) { ++ib; ++blocks; }
+    return b;
+  }
+};
+
+// code pairs of one column, natural order of inputs, into TMEM: 32 columns = two chunks of 32 inputs
+template <int CW>
+__device__ __forceinline__ void store_codes(uint32_t taddr, const uint32_t (&w)[4][Piece<CW>::WORDS], const Codec<CW>& codec) {
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    uint32_t r[32];
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int p = 0; p < 4; ++p) r[16 * c + 4 * q + p] = dequant_pair<CW>(w[q], 4 * (2 * half + c) + p, codec);
+    tmem_st32(taddr + 32 * half, r);
+  }
+}
+
+template <int CW, int NH, int TERMS, bool GRAD>
+__global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ Params p) {
+  extern __shared__ unsigned char smem_raw[];
+  using Sh = Shape<NH, TERMS>;
+  constexpr int STAGES = Sh::STAGES;
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t xring = (raw + 1023u) & ~1023u;
+  unsigned char* base = smem_raw + (xring - raw);
+  float* stage_out = reinterpret_cast<float*>(base + (size_t)STAGES * Sh::X_BYTES);
+  unsigned char* ctrl = base + (size_t)STAGES * Sh::X_BYTES + STAGE_OUT;
+  const uint32_t bar0 = smem_u32(ctrl);
+  auto xfull = [&](int s) { return bar0 + 8u * s; };
+  auto xempty = [&](int s) { return bar0 + 8u * (4 + s); };
+  auto afull = [&](int s) { return bar0 + 8u * (8 + s); };
+  auto aempty = [&](int s) { return bar0 + 8u * (12 + s); };
+  auto dfull = [&](int h) { return bar0 + 8u * (16 + h); };
+  auto dempty = [&](int h) { return bar0 + 8u * (18 + h); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl + 192);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl + 200);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) { mbar_init(xfull(s), 1); mbar_init(xempty(s), 1); }
+    for (int s = 0; s < A_STAGES; ++s) { mbar_init(afull(s), 4); mbar_init(aempty(s), 1); }
+    for (int h = 0; h < 2; ++h) { mbar_init(dfull(h), 1); mbar_init(dempty(h), 4); }
+    *abort_flag = 0;
+    mbar_fence_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot, tmem_a = tmem + 2 * NH;
+
+  const PackedView& w = p.w;
+  const int rank = p.ck == 1 ? 0 : blockIdx.x % p.ck;
+  const int ib0 = p.ck == 1 ? 0 : w.nib * rank / p.ck, ib1 = p.ck == 1 ? w.nib : w.nib * (rank + 1) / p.ck;
+  const int tiles = p.jtiles * p.ttiles, tile0 = blockIdx.x / p.ck, tstep = p.ck == 1 ? gridDim.x : tiles;
+  unsigned long long acc[NH / 2];   // NH rows of the thread's column, in pairs
+  const int h = (warp >> 2) - 2;    // which accumulator (warps 8-15)
+  const int quarter = warp & 3;
+
+  if (warp < 4) {
+    reg_dec<40>();
+    if (warp == 0 && lane == 0) {
+      int s = 0, issued = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int t = tile0; t < tiles && ok; t += tstep) {
+        const int tok0 = t / p.jtiles * (2 * NH);
+        for (int ib = ib0; ib < ib1; ++ib) {
+          if (!mbar_wait_or_abort(xempty(s), ph ^ 1u, abort_flag, SPIN)) { ok = false; break; }
+          mbar_expect_tx(xfull(s), Sh::X_BYTES);
+          const uint32_t dst = xring + (uint32_t)s * Sh::X_BYTES;
+#pragma unroll
+          for (int m = 0; m < TERMS; ++m)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) tma_load_3d(dst + (m * 2 + b) * (2 * NH * 128), &tmap, ib * KB + b * 64, tok0, m, xfull(s));
+          ++issued;
+          if (++s == STAGES) { s = 0; ph ^= 1u; }
+        }
+      }
+      if (!ok) drain_ring(bar0, STAGES, s, ph, issued, SPIN);
+    } else if (warp == 1 && lane == 0) {
+      constexpr uint32_t IDESC = idesc_bf16(128, NH, false, false);
+      int xs = 0, as = 0;
+      uint32_t xph = 0, aph = 0, dph = 1;   // dph: parity of "empty" to wait for, flips with every accumulator
+      bool ok = true;
+      for (int t = tile0; t < tiles && ok; t += tstep) {
+        Walk wk(w, ib0, ib1);
+        while (!wk.done() && ok) {
+          if (!mbar_wait_or_abort(afull(as), aph, abort_flag, SPIN) || !mbar_wait_or_abort(xfull(xs), xph, abort_flag, SPIN)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t x = xring + (uint32_t)xs * Sh::X_BYTES, a = tmem_a + as * A_COLS;
+          bool through = false;
+          while (!through) {
+            const int k0 = wk.k & (KB - 1), k1 = ((wk.seg_end() - 1) & (KB - 1)) + 1;
+            const bool first = wk.first, last = wk.last();
+#pragma unroll 1
+            for (int hh = 0; hh < 2; ++hh) {
+              if (first && !mbar_wait_or_abort(dempty(hh), dph, abort_flag, SPIN)) { ok = false; break; }
+              if (first) tc_fence_after();
+              for (int m = 0; m < TERMS; ++m)
+                for (int k = k0; k < k1; k += 16) {
+                  const uint32_t b = x + (m * 2 + (k >> 6)) * (2 * NH * 128) + hh * (NH * 128) + (k & 63) * 2;
+                  mma_ts(tmem + hh * NH, a + k / 2, desc_k_major(b), IDESC, !(first && m == 0 && k == k0));
+                }
+              if (last) mma_commit(dfull(hh));
+            }
+            if (!ok) break;
+            if (last) dph ^= 1u;
+            through = wk.next();
+          }
+          mma_commit(xempty(xs));
+          mma_commit(aempty(as));
+          if (++xs == STAGES) { xs = 0; xph ^= 1u; }
+          if (++as == A_STAGES) { as = 0; aph ^= 1u; }
+        }
+      }
+    }
+  } else if (warp < 8) {
+    reg_dec<96>();
+    constexpr int W = Piece<CW>::WORDS, AHEAD = CW == 8 ? 2 : 3;
+    const Codec<CW> codec(w);
+    uint32_t ring[AHEAD][4][W];
+    int as = 0;
+    uint32_t aph = 0;
+    bool ok = true;
+    for (int t = tile0; t < tiles && ok; t += tstep) {
+      // (columns past the last tile of 16 repeat it: their sums are not stored)
+      const int j = t % p.jtiles * BJ + quarter * 32 + lane, jt = min(j >> 4, w.njt - 1), row = j & 15;
+      const unsigned char* codes = w.codes + (long long)jt * w.nib * Piece<CW>::BLOCK;
+      auto fetch = [&](int ib, int d) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load_piece<CW>(codes + (unsigned)(ib * Piece<CW>::BLOCK), Piece<CW>::part(row, q), ring[d][q]);
+      };
+#pragma unroll
+      for (int d = 0; d < AHEAD; ++d)
+        if (ib0 + d < ib1) fetch(ib0 + d, d);
+      for (int b0 = ib0; b0 < ib1 && ok; b0 += AHEAD) {
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) {
+          const int ib = b0 + d;
+          if (ib >= ib1 || !ok) break;
+          ok = mbar_wait_or_abort(aempty(as), aph ^ 1u, abort_flag, SPIN);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          store_codes<CW>(tmem_a + as * A_COLS + ((uint32_t)(quarter * 32) << 16), ring[d], codec);
+          if (ib + AHEAD < ib1) fetch(ib + AHEAD, d);
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(afull(as));
+          if (++as == A_STAGES) { as = 0; aph ^= 1u; }
+        }
+      }
+    }
+  } else {
+    reg_inc<184>();
+    constexpr int STEP = NH < 32 ? NH : 16;
+    uint32_t dph = 0;
+    bool ok = true;
+    const float zf = (float)w.z;
+    const uint32_t td = tmem + h * NH + ((uint32_t)(quarter * 32) << 16);
+    for (int t = tile0; t < tiles && ok; t += tstep) {
+      const int jb = t % p.jtiles * BJ + quarter * 32;
+      const long long j = min((long long)jb + lane, w.d_out - 1), tok0 = (long long)(t / p.jtiles) * (2 * NH) + h * NH;
+      const float* S = p.S + tok0;
+      if (GRAD) {
+#pragma unroll
+        for (int i = 0; i < NH; i += 2) {
+          float v[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const long long tok = tok0 + i + e;
+            float d = 0.f;
+            if (tok < p.n) {
+              d = load_x(p.in.dY, p.in.xt, tok * p.in.lddy + j);
+              if (p.in.Z) d *= act_slope(load_x(p.in.Z, p.in.xt, tok * p.in.ldz + j), p.in.act);
+            }
+            v[e] = d;
+          }
+          acc[i / 2] = pack2(v[0], v[1]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NH / 2; ++i) acc[i] = 0ull;
+      }
+      float ds = 0.f;
+      Walk wk(w, ib0, ib1);
+      float a = __ldg(w.scale + (long long)min(wk.t, w.ng - 1) * w.d_out + j), b = __ldg(w.zero + (long long)min(wk.t, w.ng - 1) * w.d_out + j);
+      while (!wk.done()) {
+        if (!wk.last()) { wk.next(); continue; }
+        const int g = wk.t;
+        const bool ends = wk.group_ends();
+        wk.next();
+        float a1 = a, b1 = b;
+        if (ends && wk.t < w.ng) {
+          a1 = __ldg(w.scale + (long long)wk.t * w.d_out + j);
+          b1 = __ldg(w.zero + (long long)wk.t * w.d_out + j);
+        }
+        const float4* Sg = reinterpret_cast<const float4*>(S + g * p.ldS);
+        const unsigned long long a2 = pack2(a, a), b2 = ends ? pack2(fmaf(zf, a, b), fmaf(zf, a, b)) : 0ull;
+        unsigned long long s2 = 0ull, z2 = 0ull;
+        ok = mbar_wait_or_abort(dfull(h), dph, abort_flag, SPIN);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        dph ^= 1u;
+        tc_fence_after();
+        uint32_t d[2][STEP];
+        tmem_ld<STEP>(td, d[0]);
+#pragma unroll
+        for (int c = 0; c < NH / STEP; ++c) {
+          float4 s[STEP / 4];
+          if (!GRAD || ends) {
+#pragma unroll
+            for (int v = 0; v < STEP / 4; ++v) s[v] = __ldg(Sg + c * (STEP / 4) + v);
+          }
+          tmem_wait_ld();
+          if (c + 1 < NH / STEP) tmem_ld<STEP>(td + (c + 1) * STEP, d[(c + 1) & 1]);
+          else {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(dempty(h));
+          }
+#pragma unroll
+          for (int v = 0; v < STEP / 2; ++v) {
+            const unsigned long long P = pack2(__uint_as_float(d[c & 1][2 * v]), __uint_as_float(d[c & 1][2 * v + 1]));
+            const float4 sv = s[v / 2];
+            const unsigned long long sp = v & 1 ? pack2(sv.z, sv.w) : pack2(sv.x, sv.y);
+            unsigned long long& x = acc[c * (STEP / 2) + v];
+            if (GRAD) {
+              s2 = fma2(P, x, s2);
+              if (ends) z2 = fma2(sp, x, z2);
+            } else {
+              x = fma2(a2, P, fma2(b2, sp, x));
+            }
+          }
+        }
+        a = a1; b = b1;
+        if (GRAD) {
+          ds += lo2(s2) + hi2(s2);
+          if (ends) {
+            const long long slot = tok0 / NH;
+            const float dz = lo2(z2) + hi2(z2);
+            if (jb + lane < w.d_out) {
+              float* out = p.part + (slot * 2 * w.ng + g) * w.d_out + j;
+              out[0] = fmaf(zf, dz, ds);
+              out[(long long)w.ng * w.d_out] = dz;
+            }
+            ds = 0.f;
+          }
+        }
+      }
+      if (!GRAD && p.ck == 1 && ok) {
+        // ---- bias, activation, residual: 32 rows at a time turned round in shared memory, then 8 columns of a row per lane ----
+        float* so = stage_out + (warp - 8) * 1024;
+        const int jl = (lane & 3) * 8;
+        const bool whole = p.vec && jb + 32 <= w.d_out;
+        float bias[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bias[e] = p.ep.bias && jb + jl + e < w.d_out ? p.ep.bias[jb + jl + e] : 0.f;
+        constexpr int NB = NH < 32 ? NH : 32;
+#pragma unroll
+        for (int c = 0; c < NH / NB; ++c) {
+          if (tok0 + c * NB < p.n) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              const unsigned long long x = acc[(c * NB + i) / 2];
+              so[i * 32 + (lane ^ ((i & 7) << 2))] = i & 1 ? hi2(x) : lo2(x);
+            }
+          }
+          __syncwarp();
+#pragma unroll 1
+          for (int i = lane >> 2; i < NB; i += 8) {
+            const long long tok = tok0 + c * NB + i;
+            if (tok >= p.n) break;
+            float z[8];
+            *reinterpret_cast<float4*>(z) = *reinterpret_cast<const float4*>(so + i * 32 + (jl ^ ((i & 7) << 2)));
+            *reinterpret_cast<float4*>(z + 4) = *reinterpret_cast<const float4*>(so + i * 32 + ((jl + 4) ^ ((i & 7) << 2)));
+            write_eight(p.ep, tok, jb + jl, w.d_out, whole, bias, z);
+          }
+          __syncwarp();
+        }
+      }
+    }
+  }
+
+  if (!GRAD && p.ck > 1) {
+    // every block of the cluster has its inputs' share of the tile: sums through shared memory, the rows shared out among the blocks
+    cg::cluster_group cluster = cg::this_cluster();
+    __syncthreads();   // all instructions that read the ring are done: both accumulators were waited for
+    float* mine = reinterpret_cast<float*>(base);   // [2 NH][128]
+    const int t = tile0;
+    if (warp >= 8) {
+#pragma unroll
+      for (int i = 0; i < NH; ++i) mine[(h * NH + i) * BJ + quarter * 32 + lane] = i & 1 ? hi2(acc[i / 2]) : lo2(acc[i / 2]);
+    }
+    cluster.sync();
+    if (warp >= 8) {
+      const long long tok0 = (long long)(t / p.jtiles) * (2 * NH);
+      const int jb = t % p.jtiles * BJ;
+      for (int o = (threadIdx.x - 256) + rank * 256; o < 2 * NH * BJ; o += p.ck * 256) {
+        const long long tok = tok0 + o / BJ, j = jb + o % BJ;
+        if (tok >= p.n || j >= w.d_out) continue;
+        float s = 0.f;
+        for (int r = 0; r < p.ck; ++r) s += *cluster.map_shared_rank(mine + o, r);
+        write_out(p.ep, tok, j, s);
+      }
+    }
+    cluster.sync();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status, (int)kFlagWaitTimeout);
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_free(tmem, 512);
+  }
+}
+
+// dscale, dzero = sums of the slots' parts, ascending.
+__global__ void __launch_bounds__(256) sum_parts_kernel(const float* __restrict__ part, int slots, long long per, float* __restrict__ dscale,
+                                                        float* __restrict__ dzero) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= per) return;
+  float s = 0.f, z = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < slots; ++k) {
+    s += part[(2ll * k) * per + i];
+    z += part[(2ll * k + 1) * per + i];
+  }
+  if (dscale) dscale[i] = s;
+  if (dzero) dzero[i] = z;
+}
+
+// S[t][n] = sum of row n of X over group t (zeros for rows past n), and, where X cannot be read by TMA as it is, its bf16 terms [terms][n][kp].
+// One block per row: sums of 32 inputs first, then of the groups, both in a fixed order.
+template <int TERMS>
+__global__ void __launch_bounds__(256) prep_rows_kernel(const void* __restrict__ X, long long n, long long ldx, int d_in, int g, int ng, float* __restrict__ S,
+                                                        long long ldS, __nv_bfloat16* __restrict__ terms, long long kp, int vec) {
+  __shared__ float part[2048];
+  const long long row = blockIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (row >= n) {
+    for (int t = threadIdx.x; t < ng; t += 256) S[t * ldS + row] = 0.f;
+    return;
+  }
+  const int len = (int)kp;   // a multiple of 32, at least d_in
+  for (int c = threadIdx.x * 8; c < (len + 255) / 256 * 256; c += 256 * 8) {
+    float x[8];
+    if (TERMS == 1) {
+      const __nv_bfloat16* src = (const __nv_bfloat16*)X + row * ldx + c;
+      if (vec && c + 8 <= d_in) {
+        const uint4 y = *reinterpret_cast<const uint4*>(src);
+        const uint32_t u[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(u[e] << 16); x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u); }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = c + e < d_in ? __bfloat162float(src[e]) : 0.f;
+      }
+    } else {
+      const float* src = (const float*)X + row * ldx + c;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = c + e < d_in ? src[e] : 0.f;
+    }
+    if (terms && c < len) {
+      uint32_t t[3][8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) split3(x[e], t[0][e], t[1][e], t[2][e]);
+#pragma unroll
+      for (int m = 0; m < TERMS; ++m)
+        *reinterpret_cast<uint4*>(terms + (m * n + row) * kp + c) =
+            make_uint4(t[m][0] | t[m][1] << 16, t[m][2] | t[m][3] << 16, t[m][4] | t[m][5] << 16, t[m][6] | t[m][7] << 16);
+    }
+    float s = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    s += __shfl_xor_sync(0xffffffffu, s, 1);
+    s += __shfl_xor_sync(0xffffffffu, s, 2);
+    if ((c & 31) == 0 && c < len) part[c >> 5] = s;
+  }
+  __syncthreads();
+  const int per = ng == 1 ? (d_in + 31) / 32 : g / 32;
+  if (per >= 32) {
+    for (int t = warp; t < ng; t += 8) {
+      float s = 0.f;
+      for (int v = lane; v < per; v += 32) s += part[t * per + v];
+#pragma unroll
+      for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+      if (lane == 0) S[t * ldS + row] = s;
+    }
+  } else {
+    for (int t = threadIdx.x; t < ng; t += 256) {
+      float s = 0.f;
+      for (int v = 0; v < per; ++v) s += part[t * per + v];
+      S[t * ldS + row] = s;
+    }
+  }
+}
+
+struct Ws { size_t S, terms, part, total; long long ldS, kp; };
+Ws layout(const PackedView& w, cdq_dtype xt, long long n, bool copy, long long slots) {
+  Ws v{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
+  v.ldS = (n + 255) / 256 * 256;
+  v.kp = (w.d_in + 63) / 64 * 64;
+  v.S = take(sizeof(float) * w.ng * v.ldS);
+  if (copy) v.terms = take((size_t)(xt == CDQ_F32 ? 3 : 1) * n * v.kp * 2);
+  if (slots) v.part = take(sizeof(float) * 2 * slots * w.ng * w.d_out);
+  v.total = off;
+  return v;
+}
+
+template <int CW, int NH, int TERMS, bool GRAD>
+cudaError_t launch(const CUtensorMap& map, const Params& p, int sms, cudaStream_t st) {
+  auto kern = linear_tc_kernel<CW, NH, TERMS, GRAD>;
+  constexpr size_t bytes = Shape<NH, TERMS>::SMEM;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e != cudaSuccess) return e;
+  const int tiles = p.jtiles * p.ttiles;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(p.ck > 1 ? tiles * p.ck : tiles < sms ? tiles : sms));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)p.ck;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = p.ck > 1 ? 1 : 0;
+  count_launch();
+  return cudaLaunchKernelEx(&cfg, kern, map, p);
+}
+
+template <int CW, int NH, bool GRAD>
+cudaError_t launch_terms(const CUtensorMap& map, const Params& p, bool f32, int sms, cudaStream_t st) {
+  if (f32) return launch<CW, NH < 128 ? NH : 64, 3, GRAD>(map, p, sms, st);
+  return launch<CW, NH, 1, GRAD>(map, p, sms, st);
+}
+
+template <int CW, bool GRAD>
+cudaError_t launch_nh(const CUtensorMap& map, const Params& p, int nh, bool f32, int sms, cudaStream_t st) {
+  switch (nh) {
+    case 16: return launch_terms<CW, 16, GRAD>(map, p, f32, sms, st);
+    case 32: return launch_terms<CW, 32, GRAD>(map, p, f32, sms, st);
+    case 64: return launch_terms<CW, 64, GRAD>(map, p, f32, sms, st);
+  }
+  return launch_terms<CW, 128, GRAD>(map, p, f32, sms, st);
+}
+
+template <bool GRAD>
+cudaError_t launch_cw(int cw, const CUtensorMap& map, const Params& p, int nh, bool f32, int sms, cudaStream_t st) {
+  switch (cw) {
+    case 2: return launch_nh<2, GRAD>(map, p, nh, f32, sms, st);
+    case 3: return launch_nh<3, GRAD>(map, p, nh, f32, sms, st);
+    case 4: return launch_nh<4, GRAD>(map, p, nh, f32, sms, st);
+  }
+  return launch_nh<8, GRAD>(map, p, nh, f32, sms, st);
+}
+
+// Rows of one accumulator: the smallest that takes all rows in one tile, at most 128 (64 in fp32, whose three terms of X fill shared memory).
+int rows_half(long long n, bool f32) { return n <= 32 ? 16 : n <= 64 ? 32 : n <= 128 || f32 ? 64 : 128; }
+
+cudaError_t run(const PackedView& w, int cw, const void* X, cdq_dtype xt, long long n, long long ldx, Params& p, void* ws, bool grad, float* dscale,
+                float* dzero, cudaStream_t st) {
+  const bool f32 = xt == CDQ_F32, direct = !f32 && ldx % 8 == 0 && aligned16(X);
+  const int nh = rows_half(n, f32);
+  p.w = w; p.n = n;
+  p.jtiles = (int)((w.d_out + BJ - 1) / BJ);
+  p.ttiles = (int)((n + 2 * nh - 1) / (2 * nh));
+  const long long slots = grad ? 2ll * p.ttiles : 0;
+  const Ws L = layout(w, xt, n, true, slots);
+  char* b = (char*)ws;
+  float* S = (float*)(b + L.S);
+  __nv_bfloat16* terms = direct ? nullptr : (__nv_bfloat16*)(b + L.terms);
+  p.S = S; p.ldS = L.ldS; p.part = (float*)(b + L.part);
+  p.status = device_status_word();
+  if (!p.status) return cudaErrorInvalidSymbol;
+  int dev = 0, sms = 0;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  const int vec = f32 ? 0 : (ldx % 8 == 0 && aligned16(X));
+  if (f32) prep_rows_kernel<3><<<(unsigned)L.ldS, 256, 0, st>>>(X, n, ldx, (int)w.d_in, w.g, w.ng, S, L.ldS, terms, L.kp, vec);
+  else prep_rows_kernel<1><<<(unsigned)L.ldS, 256, 0, st>>>(X, n, ldx, (int)w.d_in, w.g, w.ng, S, L.ldS, terms, L.kp, vec);
+  count_launch();
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  CUtensorMap map;
+  if (direct) e = encode_map_3d(&map, X, w.d_in, n, 1, ldx, 0, 64, 2 * nh);
+  else e = encode_map_3d(&map, terms, L.kp, n, f32 ? 3 : 1, L.kp, L.kp * n, 64, 2 * nh);
+  if (e != cudaSuccess) return e;
+  p.ck = 1;
+  const int tiles = p.jtiles * p.ttiles;
+  if (!grad)
+    while (p.ck < 8 && tiles * p.ck * 2 <= sms && w.nib >= 4 * p.ck) p.ck *= 2;
+  e = grad ? launch_cw<true>(cw, map, p, nh, f32, sms, st) : launch_cw<false>(cw, map, p, nh, f32, sms, st);
+  if (e != cudaSuccess || !grad) return e;
+  const long long per = (long long)w.ng * w.d_out;
+  { sum_parts_kernel<<<(unsigned)((per + 255) / 256), 256, 0, st>>>(p.part, (int)slots, per, dscale, dzero); count_launch(); }
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+bool linear_tc_takes(const PackedView& w) { return w.ng == 1 || w.g % 32 == 0; }
+
+size_t linear_tc_workspace(const PackedView& w, cdq_dtype xt, long long n, bool grad) {
+  const int nh = rows_half(n, xt == CDQ_F32);
+  return layout(w, xt, n, true, grad ? 2 * ((n + 2 * nh - 1) / (2 * nh)) : 0).total;
+}
+
+cudaError_t launch_linear_tc(const PackedView& w, int cw, const void* X, cdq_dtype xt, long long n, long long ldx, const Epilogue& ep, void* ws,
+                             cudaStream_t st) {
+  Params p{};
+  p.ep = ep;
+  const int per16 = xt == CDQ_BF16 ? 8 : 4;
+  p.vec = ep.ldy % per16 == 0 && aligned16(ep.Y) && (!ep.Z || (ep.ldz % per16 == 0 && aligned16(ep.Z))) &&
+          (!ep.residual || (ep.ldr % per16 == 0 && aligned16(ep.residual)));
+  return run(w, cw, X, xt, n, ldx, p, ws, false, nullptr, nullptr, st);
+}
+
+cudaError_t launch_scale_grad_tc(const PackedView& w, int cw, const GradIn& in, float* dscale, float* dzero, void* ws, cudaStream_t st) {
+  Params p{};
+  p.in = in;
+  return run(w, cw, in.X, in.xt, in.n, in.ldx, p, ws, true, dscale, dzero, st);
+}
+
+}  // namespace cdq

@@ -26,11 +26,14 @@ template <int CW> struct Ring {
 };
 
 // P += codes of 32 inputs (chunk c of the block) x rows; FIRST: P = instead.  xs: row 0 of the staged rows at the chunk's first input; row_at: where
-// the lane's row of every tile of eight starts, plus 8 (lane % 4).
+// the lane's row of every tile of eight starts, plus 8 (lane % 4).  One term (bf16): S, the sums of the rows, comes from the same instruction with ones
+// on the left, and lies where P lies; that costs 8 more instructions per block of 2048 codes, while summing every row as it is staged costs each thread
+// block the whole of X (8 rows x 4096 inputs: 8 us against 1).
 template <int CW, int NT, int TERMS, bool FIRST>
 __device__ __forceinline__ void mma_chunk(const uint32_t* w, int c, const Codec<CW>& k, const __nv_bfloat16* xs, const int (&row_at)[NT], int term_at,
-                                          float (&P)[NT][4]) {
+                                          float (&P)[NT][4], float (&S)[NT][4]) {
   constexpr int W = Piece<CW>::WORDS;
+  constexpr uint32_t ONES = 0x3f803f80u;
   uint32_t a[4], b[4];
 #pragma unroll
   for (int p = 0; p < 4; ++p) { a[p] = dequant_pair<CW>(w, 4 * c + p, k); b[p] = dequant_pair<CW>(w + W, 4 * c + p, k); }
@@ -41,57 +44,61 @@ __device__ __forceinline__ void mma_chunk(const uint32_t* w, int c, const Codec<
       const uint4 x = *reinterpret_cast<const uint4*>(xs + row_at[t] + m * term_at);
       if (FIRST && m == 0) mma_16816_new(P[t], a[0], b[0], a[1], b[1], x.x, x.y);
       else mma_16816(P[t], a[0], b[0], a[1], b[1], x.x, x.y);
+      if (TERMS == 1) {
+        if (FIRST) mma_16816_new(S[t], ONES, ONES, ONES, ONES, x.x, x.y);
+        else mma_16816(S[t], ONES, ONES, ONES, ONES, x.x, x.y);
+      }
       mma_16816(P[t], a[2], b[2], a[3], b[3], x.z, x.w);
+      if (TERMS == 1) mma_16816(S[t], ONES, ONES, ONES, ONES, x.z, x.w);
     }
 }
 
-// acc += a P + (b + z a) S for the group's scales and zeros of the lane's two columns; sums: S of the rows, at the lane's first (of tiles 8 apart).
-template <int NT>
-__device__ __forceinline__ void promote(const float (&s)[4], float z, const float* sums, const float (&P)[NT][4], float (&acc)[NT][4]) {
-  const float b0 = fmaf(z, s[0], s[1]), b1 = fmaf(z, s[2], s[3]);
+// S of the lane's rows 2 q, 2 q + 1 of every tile of eight from where stage_rows left them (more terms than one).
+template <int NT, int TERMS>
+__device__ __forceinline__ void fetch_sums(const float* sums, float (&S)[NT][4]) {
+  if (TERMS > 1) {
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const float2 S = *reinterpret_cast<const float2*>(sums + 8 * t);
-    acc[t][0] = fmaf(s[0], P[t][0], fmaf(b0, S.x, acc[t][0]));
-    acc[t][1] = fmaf(s[0], P[t][1], fmaf(b0, S.y, acc[t][1]));
-    acc[t][2] = fmaf(s[2], P[t][2], fmaf(b1, S.x, acc[t][2]));
-    acc[t][3] = fmaf(s[2], P[t][3], fmaf(b1, S.y, acc[t][3]));
+    for (int t = 0; t < NT; ++t) { S[t][0] = sums[8 * t]; S[t][1] = sums[8 * t + 1]; }
   }
 }
 
-// Stages inputs [i0, i0 + len) of `rows` rows into shared memory as bf16 (fp32 as three terms), zeros past d_in, and their sums over every UNIT (32 or
-// 128) inputs.  len is a multiple of 128.  Row r of term m starts at m * term_at + r * pitch; the sum of row r over unit u is sums[u * spitch + r].
+// acc += a P + (b + z a) S for the group's scales and zeros of the lane's two columns.
+template <int NT>
+__device__ __forceinline__ void promote(const float (&s)[4], float z, const float (&S)[NT][4], const float (&P)[NT][4], float (&acc)[NT][4]) {
+  const float b0 = fmaf(z, s[0], s[1]), b1 = fmaf(z, s[2], s[3]);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    acc[t][0] = fmaf(s[0], P[t][0], fmaf(b0, S[t][0], acc[t][0]));
+    acc[t][1] = fmaf(s[0], P[t][1], fmaf(b0, S[t][1], acc[t][1]));
+    acc[t][2] = fmaf(s[2], P[t][2], fmaf(b1, S[t][0], acc[t][2]));
+    acc[t][3] = fmaf(s[2], P[t][3], fmaf(b1, S[t][1], acc[t][3]));
+  }
+}
+
+// Stages inputs [i0, i0 + len) of `rows` rows into shared memory as bf16, zeros past d_in; len is a multiple of 128.  Row r of term m starts at
+// m * term_at + r * pitch.  fp32 becomes three terms, and its sums over every UNIT (32 or 128) inputs are kept: of row r over unit u at
+// sums[u * spitch + r].  (What bulk copies cannot take; they stage whole bf16 rows that start on 16 bytes.)
 template <int TERMS, int UNIT>
 __device__ __forceinline__ void stage_rows(__nv_bfloat16* xs, int pitch, int term_at, float* sums, int spitch, const void* X, long long ldx,
-                                           long long d_in, int rows, long long i0, int len, bool vec) {
+                                           long long d_in, int rows, long long i0, int len) {
   const unsigned half = 0xffffu << (threadIdx.x & 16);   // the 16 lanes of a block of 128 inputs come and go together
   for (int r = 0; r < rows; ++r)
     for (int c = threadIdx.x * 8; c < len; c += blockDim.x * 8) {
-      const long long i = i0 + c;
+      const long long left = d_in - i0 - c, at = r * ldx + i0 + c;
       uint32_t x[TERMS][4];
       float s = 0.f;
-      if (TERMS == 1) {
-        const __nv_bfloat16* src = (const __nv_bfloat16*)X + r * ldx + i;
-        if (vec && i + 8 <= d_in) {
-          const uint4 y = *reinterpret_cast<const uint4*>(src);
-          x[0][0] = y.x; x[0][1] = y.y; x[0][2] = y.z; x[0][3] = y.w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (TERMS == 1) {
+          const __nv_bfloat16* src = (const __nv_bfloat16*)X + at;
+          const uint32_t lo = 2 * e < left ? __bfloat16_as_ushort(src[2 * e]) : 0, hi = 2 * e + 1 < left ? __bfloat16_as_ushort(src[2 * e + 1]) : 0;
+          x[0][e] = lo | hi << 16;
         } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t lo = i + 2 * e < d_in ? __bfloat16_as_ushort(src[2 * e]) : 0, hi = i + 2 * e + 1 < d_in ? __bfloat16_as_ushort(src[2 * e + 1]) : 0;
-            x[0][e] = lo | hi << 16;
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s += __uint_as_float(x[0][e] << 16) + __uint_as_float(x[0][e] & 0xffff0000u);
-      } else {
-        const float* src = (const float*)X + r * ldx + i;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
+          const float* src = (const float*)X + at;
           uint32_t t[2][3];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const float y = i + 2 * e + h < d_in ? src[2 * e + h] : 0.f;
+            const float y = 2 * e + h < left ? src[2 * e + h] : 0.f;
             s += y;
             split3(y, t[h][0], t[h][1], t[h][2]);
           }
@@ -102,9 +109,11 @@ __device__ __forceinline__ void stage_rows(__nv_bfloat16* xs, int pitch, int ter
 #pragma unroll
       for (int m = 0; m < TERMS; ++m)
         *reinterpret_cast<uint4*>(xs + m * term_at + r * pitch + c) = make_uint4(x[m][0], x[m][1], x[m][2], x[m][3]);
+      if (TERMS > 1) {
 #pragma unroll
-      for (int d = 1; d < UNIT / 8; d *= 2) s += __shfl_xor_sync(half, s, d);
-      if (c % UNIT == 0) sums[c / UNIT * spitch + r] = s;
+        for (int d = 1; d < UNIT / 8; d *= 2) s += __shfl_xor_sync(half, s, d);
+        if (c % UNIT == 0) sums[c / UNIT * spitch + r] = s;
+      }
     }
 }
 

@@ -1,0 +1,165 @@
+// tcgen05, TMEM and TMA instructions as the kernels of packed layers use them.
+#pragma once
+
+#include <cuda.h>
+
+#include "async_copy.cuh"
+#include "packed.cuh"
+
+namespace cdq {
+
+template <int R> __device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
+template <int R> __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
+
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t cols) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t base, uint32_t cols) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+template <int N> __device__ __forceinline__ void tmem_ld(uint32_t a, uint32_t (&r)[N]);
+template <> __device__ __forceinline__ void tmem_ld<16>(uint32_t a, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                 "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(a)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t a, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(a),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+      "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+
+// Instruction descriptor: fp32 sums, bf16 operands; a_mn / b_mn: the operand's rows (not its K) lie side by side.
+__host__ __device__ constexpr uint32_t idesc_bf16(int m, int n, bool a_mn, bool b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+// Shared-memory operand with 128-byte rows along K and the 128-byte swizzle: groups of eight rows 1 KB apart.
+__device__ __forceinline__ uint64_t desc_k_major(uint32_t a) {
+  return (uint64_t)((a & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// Left operand in TMEM.
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+// A producer that gives up lets the copies that it asked for land before its block goes away (bounded).  full0: the ring's first barrier.
+__device__ __forceinline__ void drain_ring(uint32_t full0, int stages, int stage, uint32_t phase, int issued, uint32_t spin) {
+  const int pending = issued < stages ? issued : stages;
+  for (int q = 0; q < pending; ++q) {
+    int s = stage - 1 - q;
+    uint32_t ph = phase;
+    if (s < 0) { s += stages; ph ^= 1u; }
+    for (uint32_t it = 0; it < spin; ++it)
+      if (mbar_try_wait(full0 + 8u * s, ph)) break;
+  }
+}
+
+// ---- pairs of fp32 in one register pair ----
+__device__ __forceinline__ unsigned long long pack2(float lo, float hi) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float lo2(unsigned long long v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float hi2(unsigned long long v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+// Eight columns of a row: bias, activation, residual, stores of 16 bytes where `whole`.
+__device__ __forceinline__ void write_eight(const Epilogue& e, long long tok, long long j, long long d_out, bool whole, const float (&bias)[8], float (&z)[8]) {
+  if (!whole) {
+#pragma unroll
+    for (int v = 0; v < 8; ++v)
+      if (j + v < d_out) write_out(e, tok, j + v, z[v]);
+    return;
+  }
+  auto store = [&](void* to, long long at, const float (&x)[8]) {
+    if (e.xt == CDQ_BF16) {
+      uint32_t r[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * v], x[2 * v + 1]);
+        r[v] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+      *reinterpret_cast<uint4*>((__nv_bfloat16*)to + at) = make_uint4(r[0], r[1], r[2], r[3]);
+    } else {
+      float* f = (float*)to + at;
+      *reinterpret_cast<float4*>(f) = make_float4(x[0], x[1], x[2], x[3]);
+      *reinterpret_cast<float4*>(f + 4) = make_float4(x[4], x[5], x[6], x[7]);
+    }
+  };
+  float y[8];
+#pragma unroll
+  for (int v = 0; v < 8; ++v) y[v] = z[v] += bias[v];
+  if (e.Z) store(e.Z, tok * e.ldz + j, z);
+  switch (e.act) {   // outside the loop over the columns
+    case CDQ_ACT_NONE: break;
+    case CDQ_ACT_RELU:
+#pragma unroll
+      for (int v = 0; v < 8; ++v) y[v] = act_of(z[v], CDQ_ACT_RELU);
+      break;
+    case CDQ_ACT_SILU:
+#pragma unroll
+      for (int v = 0; v < 8; ++v) y[v] = act_of(z[v], CDQ_ACT_SILU);
+      break;
+    case CDQ_ACT_GELU:
+#pragma unroll
+      for (int v = 0; v < 8; ++v) y[v] = act_of(z[v], CDQ_ACT_GELU);
+      break;
+    default:
+#pragma unroll
+      for (int v = 0; v < 8; ++v) y[v] = act_of(z[v], CDQ_ACT_GELU_TANH);
+  }
+  if (e.residual) {
+    if (e.xt == CDQ_BF16) {
+      const uint4 r = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)e.residual + tok * e.ldr + j);
+      const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+      for (int v = 0; v < 4; ++v) { y[2 * v] += __uint_as_float(u[v] << 16); y[2 * v + 1] += __uint_as_float(u[v] & 0xffff0000u); }
+    } else {
+      const float* f = (const float*)e.residual + tok * e.ldr + j;
+#pragma unroll
+      for (int v = 0; v < 8; ++v) y[v] += f[v];
+    }
+  }
+  store(e.Y, tok * e.ldy + j, y);
+}
+
+// Tensor map of bf16 planes [z][y][x]: row stride ldx and plane stride ldz in entries; boxes of bx x by entries, 128-byte swizzle, zeros outside.
+cudaError_t encode_map_3d(CUtensorMap* map, const void* base, long long x, long long y, long long z, long long ldx, long long ldz, int bx, int by);
+
+}  // namespace cdq
