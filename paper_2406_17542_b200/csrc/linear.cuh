@@ -30,6 +30,11 @@ cudaError_t launch_linear_tc(const PackedView& w, int cw, const void* X, cdq_dty
                              cudaStream_t st);
 cudaError_t launch_scale_grad_tc(const PackedView& w, int cw, const GradIn& in, float* dscale, float* dzero, void* ws, cudaStream_t st);
 
+// linear_dx.cu: the same layers
+bool dx_tc_takes(const PackedView& w);
+size_t dx_tc_workspace(const PackedView& w, cdq_dtype xt, long long n);
+cudaError_t launch_dx_tc(const PackedView& w, int cw, const GradIn& in, void* dX, long long lddx, void* ws, cudaStream_t st);
+
 // linear_skinny.cu: up to 16 rows, one group or groups that are multiples of 32
 bool linear_skinny_takes(const PackedView& w, long long n);
 cudaError_t launch_linear_skinny(const PackedView& w, int cw, const void* X, long long n, long long ldx, const Epilogue& ep, cudaStream_t st);

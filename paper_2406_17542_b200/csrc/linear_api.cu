@@ -108,7 +108,9 @@ cdq_status cdq_linear(const cdq_packed_layer* layer, const void* X, cdq_dtype xt
 size_t cdq_linear_backward_workspace_bytes(const cdq_packed_layer* layer, cdq_dtype xt, long long n) {
   if (check_packed(layer) != CDQ_OK || !valid_type(xt) || n < 1 || n > kMaxRows) return 0;
   const PackedView w = view_of(*layer);
-  return linear_tc_takes(w) ? linear_tc_workspace(w, xt, n, true) : 0;
+  if (!linear_tc_takes(w)) return 0;
+  const size_t a = linear_tc_workspace(w, xt, n, true), b = dx_tc_workspace(w, xt, n);   // one after the other in the same place
+  return a > b ? a : b;
 }
 
 cdq_status cdq_linear_backward(const cdq_packed_layer* layer, const void* dY, cdq_dtype xt, long long n, long long lddy, const void* X, long long ldx,
@@ -133,7 +135,10 @@ cdq_status cdq_linear_backward(const cdq_packed_layer* layer, const void* dY, cd
     if (linear_tc_takes(w)) CDQ_CUDA(launch_scale_grad_tc(w, cw, in, dscale, dzero, ws, st));
     else CDQ_CUDA(launch_scale_grad_simple(w, cw, in, dscale, dzero, st));
   }
-  if (dX) CDQ_CUDA(launch_dx_simple(w, cw, in, dX, lddx, st));
+  if (dX) {
+    if (dx_tc_takes(w)) CDQ_CUDA(launch_dx_tc(w, cw, in, dX, lddx, ws, st));
+    else CDQ_CUDA(launch_dx_simple(w, cw, in, dX, lddx, st));
+  }
   return CDQ_OK;
 }
 

@@ -1,0 +1,434 @@
+// dX = dZ W_hat^T, dZ = dY * act'(Z): the gradient of a packed layer's product for its inputs, on the 5th-generation tensor cores.
+//
+//   D[i, n] = sum_j W_hat[i, j] dZ[n, j],   W_hat[i, j] = a_t(i),j Q[i, j] + b_t(i),j
+//
+// The scales run along the sum, so they cannot wait for it: W_hat is formed in fp32 and rounded to bf16 for the tensor core (2^-9 of a weight, half a
+// step of bf16, as any bf16 product of the layer would take it); so is dZ, unless it is dY itself.  fp32: both as three bf16 terms, the six products
+// that reach 2^-24.
+//
+//   * tile 128 inputs x 2 NH rows, 64 columns of the layer per step; dZ by TMA (128-byte swizzle), W_hat from the packed codes by four warps into
+//     shared memory with the inputs side by side (a piece is four runs of 8 inputs of one column: four 16-byte stores, the tile's rows are columns);
+//   * two TMEM accumulators; warps 8-15 drain them into registers (a sum longer than FLUSH columns in several parts, added in fp32: the tensor core
+//     truncates) and write dX;
+//   * few tiles: a cluster shares the columns out and adds its sums over shared memory.
+#include <cuda.h>
+
+#include "linear.cuh"
+#include "tc5.cuh"
+
+namespace cdq {
+namespace {
+
+constexpr int BI = 128, KB = 64, THREADS = 512;
+constexpr uint32_t SPIN = 1u << 24;
+constexpr int A_TERM = BI * KB * 2;             // 16 KB
+constexpr int STAGE_OUT = 8 * 32 * 32 * 4;
+
+template <int NH, int TERMS> struct Shape {
+  static constexpr int B_TERM = 2 * NH * KB * 2;
+  static constexpr int BYTES = TERMS * (A_TERM + B_TERM);
+  static constexpr int STAGES = 196608 / BYTES < 4 ? 196608 / BYTES : 4;
+  static constexpr int FLUSH = TERMS == 1 ? 64 : 4;   // steps behind one accumulator: 4096 columns, 256 in fp32
+  static constexpr size_t RAW = 1024 + (size_t)STAGES * BYTES + STAGE_OUT + 512;
+  static constexpr size_t SMEM = RAW < 120 * 1024 ? 120 * 1024 : RAW;
+};
+
+struct Params {
+  PackedView w;
+  Epilogue ep;     // Y: dX
+  long long n;
+  int itiles, ttiles, ck, vec, steps;
+  int* status;
+};
+
+// MN-major operand with the 128-byte swizzle: blocks of 64 inputs 8 KB apart, groups of eight columns of the layer 1 KB apart.
+__device__ __forceinline__ uint64_t desc_mn_major(uint32_t a) {
+  return (uint64_t)((a & 0x3FFFFu) >> 4) | ((uint64_t)(8192 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+template <int CW, int NH, int TERMS, bool CHUNKS>
+__global__ void __launch_bounds__(THREADS, 1) linear_dx_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ Params p) {
+  extern __shared__ unsigned char smem_raw[];
+  using Sh = Shape<NH, TERMS>;
+  constexpr int STAGES = Sh::STAGES;
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t ring = (raw + 1023u) & ~1023u;
+  unsigned char* base = smem_raw + (ring - raw);
+  float* stage_out = reinterpret_cast<float*>(base + (size_t)STAGES * Sh::BYTES);
+  unsigned char* ctrl = base + (size_t)STAGES * Sh::BYTES + STAGE_OUT;
+  const uint32_t bar0 = smem_u32(ctrl);
+  auto bfull = [&](int s) { return bar0 + 8u * s; };
+  auto empty = [&](int s) { return bar0 + 8u * (4 + s); };
+  auto afull = [&](int s) { return bar0 + 8u * (8 + s); };
+  auto dfull = [&](int b) { return bar0 + 8u * (12 + b); };
+  auto dempty = [&](int b) { return bar0 + 8u * (14 + b); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl + 192);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl + 200);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) { mbar_init(bfull(s), 1); mbar_init(empty(s), 1); mbar_init(afull(s), 4); }
+    for (int b = 0; b < 2; ++b) { mbar_init(dfull(b), 1); mbar_init(dempty(b), 8); }
+    *abort_flag = 0;
+    mbar_fence_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  const PackedView& w = p.w;
+  const int rank = p.ck == 1 ? 0 : blockIdx.x % p.ck;
+  const int k0 = p.ck == 1 ? 0 : (int)((long long)p.steps * rank / p.ck), k1 = p.ck == 1 ? p.steps : (int)((long long)p.steps * (rank + 1) / p.ck);
+  const int tiles = p.itiles * p.ttiles, tile0 = blockIdx.x / p.ck, tstep = p.ck == 1 ? gridDim.x : tiles;
+  const int h = (warp >> 2) - 2, quarter = warp & 3;
+
+  if (warp < 4) {
+    reg_dec<40>();
+    if (warp == 0 && lane == 0) {
+      int s = 0, issued = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int t = tile0; t < tiles && ok; t += tstep) {
+        const int tok0 = t / p.itiles * (2 * NH);
+        for (int k = k0; k < k1; ++k) {
+          if (!mbar_wait_or_abort(empty(s), ph ^ 1u, abort_flag, SPIN)) { ok = false; break; }
+          mbar_expect_tx(bfull(s), TERMS * Sh::B_TERM);
+          const uint32_t dst = ring + (uint32_t)s * Sh::BYTES + TERMS * A_TERM;
+#pragma unroll
+          for (int m = 0; m < TERMS; ++m) tma_load_3d(dst + m * Sh::B_TERM, &tmap, k * KB, tok0, m, bfull(s));
+          ++issued;
+          if (++s == STAGES) { s = 0; ph ^= 1u; }
+        }
+      }
+      if (!ok) drain_ring(bar0, STAGES, s, ph, issued, SPIN);
+    } else if (warp == 1) {
+      constexpr uint32_t IDESC = idesc_bf16(128, 2 * NH, true, false);
+      const bool leader = elect_one();
+      int s = 0, buf = 0;
+      uint32_t ph = 0, dph = 0;
+      bool ok = true;
+      for (int t = tile0; t < tiles && ok; t += tstep)
+        for (int kc = k0; kc < k1 && ok; kc += Sh::FLUSH) {
+          ok = __all_sync(0xffffffffu, mbar_wait_or_abort(dempty(buf), dph ^ 1u, abort_flag, SPIN));
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t d = tmem + buf * (2 * NH);
+          const int kl = min(k1, kc + Sh::FLUSH);
+          for (int k = kc; k < kl; ++k) {
+            ok = mbar_wait_or_abort(afull(s), ph, abort_flag, SPIN) && mbar_wait_or_abort(bfull(s), ph, abort_flag, SPIN);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t at = ring + (uint32_t)s * Sh::BYTES;
+            const uint64_t a = desc_mn_major(at), b = desc_k_major(at + TERMS * A_TERM);   // addresses count in units of 16 bytes
+            if (leader) {
+#pragma unroll
+              for (int ma = 0; ma < TERMS; ++ma)
+#pragma unroll
+                for (int mb = 0; mb + ma < TERMS; ++mb)
+#pragma unroll
+                  for (int kk = 0; kk < KB / 16; ++kk)
+                    mma_ss(d, a + (ma * A_TERM + kk * 2048) / 16, b + (mb * Sh::B_TERM + kk * 32) / 16, IDESC, ma + mb + kk > 0 || k > kc);
+              mma_commit(empty(s));
+              if (k + 1 == kl) mma_commit(dfull(buf));
+            }
+            __syncwarp();
+            if (++s == STAGES) { s = 0; ph ^= 1u; }
+          }
+          if (!ok) break;
+          if (++buf == 2) { buf = 0; dph ^= 1u; }
+        }
+    }
+  } else if (warp < 8) {
+    reg_dec<104>();
+    // warp q of the four makes quarter q of 64 columns: lane, lane + 32
+    constexpr int W = Piece<CW>::WORDS, PLACES = Codec<CW>::PLACES;
+    const Codec<CW> codec(w);
+    const int q = warp - 4;
+    int s = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    uint32_t cd[2][W];
+    float sc[2][CHUNKS ? 4 : 1], ze[2][CHUNKS ? 4 : 1];
+    auto fetch = [&](int ib, int k) {
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const long long j = (long long)k * KB + 32 * v + lane, jc = min(j, w.d_out - 1);
+        const int jt = min((int)(j >> 4), w.njt - 1);
+        load_piece<CW>(w.codes + ((long long)jt * w.nib + ib) * Piece<CW>::BLOCK, Piece<CW>::part((int)(j & 15), q), cd[v]);
+#pragma unroll
+        for (int c = 0; c < (CHUNKS ? 4 : 1); ++c) {
+          const long long t = w.ng == 1 ? 0 : min((ib * 128 + 32 * c) / w.g, w.ng - 1);
+          sc[v][c] = __ldg(w.scale + t * w.d_out + jc);
+          ze[v][c] = __ldg(w.zero + t * w.d_out + jc);
+        }
+      }
+    };
+    for (int t = tile0; t < tiles && ok; t += tstep) {
+      const int ib = t % p.itiles;
+      fetch(ib, k0);
+      for (int k = k0; k < k1; ++k) {
+        uint32_t now[2][W];
+        float a[2][CHUNKS ? 4 : 1], b[2][CHUNKS ? 4 : 1];
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+#pragma unroll
+          for (int x = 0; x < W; ++x) now[v][x] = cd[v][x];
+#pragma unroll
+          for (int c = 0; c < (CHUNKS ? 4 : 1); ++c) { a[v][c] = sc[v][c]; b[v][c] = ze[v][c]; }
+        }
+        if (k + 1 < k1) fetch(ib, k + 1);
+        ok = mbar_wait_or_abort(empty(s), ph ^ 1u, abort_flag, SPIN);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t dst = ring + (uint32_t)s * Sh::BYTES;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int jr = 32 * v + lane;
+          // columns past the layer's: dZ is zero there (outside the tensor map or its padding), W_hat finite
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const float av = a[v][CHUNKS ? c : 0], bv = fmaf((float)w.z, av, b[v][CHUNKS ? c : 0]);
+            uint32_t r[TERMS][4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t pair = dequant_pair<CW>(now[v], 4 * c + x, codec);   // code - z, twice
+              const float lo = fmaf(av, __uint_as_float(pair << 16), bv), hi = fmaf(av, __uint_as_float(pair & 0xffff0000u), bv);
+              if (TERMS == 1) {
+                const __nv_bfloat162 y = __floats2bfloat162_rn(lo, hi);
+                r[0][x] = *reinterpret_cast<const uint32_t*>(&y);
+              } else {
+                uint32_t tl[3], th[3];
+                split3(lo, tl[0], tl[1], tl[2]);
+                split3(hi, th[0], th[1], th[2]);
+#pragma unroll
+                for (int m = 0; m < TERMS; ++m) r[m][x] = tl[m] | th[m] << 16;
+              }
+            }
+            const int chunk = 4 * c + q;   // run of 8 inputs
+            const uint32_t at = dst + (chunk >> 3) * 8192 + jr * 128 + (((chunk & 7) ^ (jr & 7)) << 4);
+#pragma unroll
+            for (int m = 0; m < TERMS; ++m)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + m * A_TERM), "r"(r[m][0]), "r"(r[m][1]), "r"(r[m][2]), "r"(r[m][3])
+                           : "memory");
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(afull(s));
+        if (++s == STAGES) { s = 0; ph ^= 1u; }
+      }
+    }
+  } else {
+    reg_inc<184>();
+    unsigned long long acc[NH / 2];   // NH rows of the thread's column, in pairs
+    constexpr int STEP = 16;
+    int buf = 0;
+    uint32_t dph = 0;
+    bool ok = true;
+    for (int t = tile0; t < tiles && ok; t += tstep) {
+      const int jb = t % p.itiles * BI + quarter * 32;
+      const long long tok0 = (long long)(t / p.itiles) * (2 * NH) + h * NH;
+#pragma unroll
+      for (int i = 0; i < NH / 2; ++i) acc[i] = 0ull;
+      const unsigned long long one = pack2(1.f, 1.f);
+      for (int kc = k0; kc < k1; kc += Sh::FLUSH) {
+        ok = mbar_wait_or_abort(dfull(buf), dph, abort_flag, SPIN);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t td = tmem + buf * (2 * NH) + h * NH + ((uint32_t)(quarter * 32) << 16);
+        uint32_t d[2][STEP];
+        tmem_ld<STEP>(td, d[0]);
+#pragma unroll
+        for (int c = 0; c < NH / STEP; ++c) {
+          tmem_wait_ld();
+          if (c + 1 < NH / STEP) tmem_ld<STEP>(td + (c + 1) * STEP, d[(c + 1) & 1]);
+          else {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(dempty(buf));
+          }
+#pragma unroll
+          for (int v = 0; v < STEP / 2; ++v) {
+            unsigned long long& x = acc[c * (STEP / 2) + v];
+            x = fma2(one, pack2(__uint_as_float(d[c & 1][2 * v]), __uint_as_float(d[c & 1][2 * v + 1])), x);
+          }
+        }
+        if (++buf == 2) { buf = 0; dph ^= 1u; }
+      }
+      if (p.ck == 1 && ok) {
+        float* so = stage_out + (warp - 8) * 1024;
+        const int jl = (lane & 3) * 8;
+        const bool whole = p.vec && jb + 32 <= w.d_in;
+        const float none[8] = {};
+        constexpr int NB = NH < 32 ? NH : 32;
+#pragma unroll
+        for (int c = 0; c < NH / NB; ++c) {
+          if (tok0 + c * NB < p.n) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              const unsigned long long x = acc[(c * NB + i) / 2];
+              so[i * 32 + (lane ^ ((i & 7) << 2))] = i & 1 ? hi2(x) : lo2(x);
+            }
+          }
+          __syncwarp();
+#pragma unroll 1
+          for (int i = lane >> 2; i < NB; i += 8) {
+            const long long tok = tok0 + c * NB + i;
+            if (tok >= p.n) break;
+            float z[8];
+            *reinterpret_cast<float4*>(z) = *reinterpret_cast<const float4*>(so + i * 32 + (jl ^ ((i & 7) << 2)));
+            *reinterpret_cast<float4*>(z + 4) = *reinterpret_cast<const float4*>(so + i * 32 + ((jl + 4) ^ ((i & 7) << 2)));
+            write_eight(p.ep, tok, jb + jl, w.d_in, whole, none, z);
+          }
+          __syncwarp();
+        }
+      }
+    }
+    if (p.ck > 1) {   // every block of the cluster has its share of the one tile
+      const int t = tile0;
+      cluster_sum<NH>(reinterpret_cast<float*>(base), acc, h, quarter * 32 + lane, rank, p.ck, [&](int i, int c, float s) {
+        const long long tok = (long long)(t / p.itiles) * (2 * NH) + i, o = (long long)(t % p.itiles) * BI + c;
+        if (tok < p.n && o < w.d_in) write_out(p.ep, tok, o, s);
+      });
+    }
+  }
+  if (warp < 8 && p.ck > 1) cluster_sum_others();
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status, (int)kFlagWaitTimeout);
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_free(tmem, 512);
+  }
+}
+
+// dZ = dY act'(Z) as bf16 [n][kp] (fp32: [3][n][kp], its three terms), zeros in the columns past d_out.
+template <int TERMS>
+__global__ void __launch_bounds__(256) dz_kernel(GradIn in, long long d_out, long long kp, __nv_bfloat16* __restrict__ out) {
+  const long long row = blockIdx.y, c = ((long long)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (c >= kp) return;
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float d = 0.f;
+    if (c + e < d_out) {
+      d = load_x(in.dY, in.xt, row * in.lddy + c + e);
+      if (in.Z) d *= act_slope(load_x(in.Z, in.xt, row * in.ldz + c + e), in.act);
+    }
+    x[e] = d;
+  }
+  uint32_t r[TERMS][4];
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    if (TERMS == 1) {
+      const __nv_bfloat162 y = __floats2bfloat162_rn(x[2 * v], x[2 * v + 1]);
+      r[0][v] = *reinterpret_cast<const uint32_t*>(&y);
+    } else {
+      uint32_t a[3], b[3];
+      split3(x[2 * v], a[0], a[1], a[2]);
+      split3(x[2 * v + 1], b[0], b[1], b[2]);
+#pragma unroll
+      for (int m = 0; m < TERMS; ++m) r[m][v] = a[m] | b[m] << 16;
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < TERMS; ++m) *reinterpret_cast<uint4*>(out + (m * in.n + row) * kp + c) = make_uint4(r[m][0], r[m][1], r[m][2], r[m][3]);
+}
+
+int rows_half(long long n, bool f32) { return n <= 32 ? 16 : n <= 64 ? 32 : n <= 128 || f32 ? 64 : 128; }
+
+template <int CW, int NH, int TERMS>
+cudaError_t launch(const CUtensorMap& map, const Params& p, int sms, cudaStream_t st) {
+  const bool chunks = p.w.ng > 1 && p.w.g % 128;
+  auto kern = chunks ? linear_dx_kernel<CW, NH, TERMS, true> : linear_dx_kernel<CW, NH, TERMS, false>;
+  constexpr size_t bytes = Shape<NH, TERMS>::SMEM;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e != cudaSuccess) return e;
+  const int tiles = p.itiles * p.ttiles;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(p.ck > 1 ? tiles * p.ck : tiles < sms ? tiles : sms));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)p.ck;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = p.ck > 1 ? 1 : 0;
+  count_launch();
+  return cudaLaunchKernelEx(&cfg, kern, map, p);
+}
+
+template <int CW>
+cudaError_t launch_nh(const CUtensorMap& map, const Params& p, int nh, bool f32, int sms, cudaStream_t st) {
+  switch (nh) {
+    case 16: return f32 ? launch<CW, 16, 3>(map, p, sms, st) : launch<CW, 16, 1>(map, p, sms, st);
+    case 32: return f32 ? launch<CW, 32, 3>(map, p, sms, st) : launch<CW, 32, 1>(map, p, sms, st);
+    case 64: return f32 ? launch<CW, 64, 3>(map, p, sms, st) : launch<CW, 64, 1>(map, p, sms, st);
+  }
+  return launch<CW, 128, 1>(map, p, sms, st);
+}
+
+}  // namespace
+
+bool dx_tc_takes(const PackedView& w) { return w.ng == 1 || w.g % 32 == 0; }
+
+size_t dx_tc_workspace(const PackedView& w, cdq_dtype xt, long long n) {
+  return align_up((size_t)(xt == CDQ_F32 ? 3 : 1) * n * ((w.d_out + 63) / 64 * 64) * 2);
+}
+
+cudaError_t launch_dx_tc(const PackedView& w, int cw, const GradIn& in, void* dX, long long lddx, void* ws, cudaStream_t st) {
+  const bool f32 = in.xt == CDQ_F32, direct = !f32 && !in.Z && in.lddy % 8 == 0 && aligned16(in.dY);
+  const int nh = rows_half(in.n, f32);
+  Params p{};
+  p.w = w; p.n = in.n;
+  p.ep.Y = dX; p.ep.ldy = lddx; p.ep.act = CDQ_ACT_NONE; p.ep.xt = in.xt;
+  p.vec = lddx % (f32 ? 4 : 8) == 0 && aligned16(dX);
+  p.itiles = (int)((w.d_in + BI - 1) / BI);
+  p.ttiles = (int)((in.n + 2 * nh - 1) / (2 * nh));
+  p.steps = (int)((w.d_out + KB - 1) / KB);
+  p.status = device_status_word();
+  if (!p.status) return cudaErrorInvalidSymbol;
+  int dev = 0, sms = 0;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  const long long kp = (w.d_out + 63) / 64 * 64;
+  CUtensorMap map;
+  cudaError_t e;
+  if (direct) {
+    e = encode_map_3d(&map, in.dY, w.d_out, in.n, 1, in.lddy, 0, 64, 2 * nh);
+  } else {
+    __nv_bfloat16* dz = (__nv_bfloat16*)ws;
+    for (long long r0 = 0; r0 < in.n; r0 += 65535) {   // rows are a grid dimension
+      GradIn part = in;
+      part.n = in.n;
+      const long long rows = in.n - r0 < 65535 ? in.n - r0 : 65535;
+      const size_t es = f32 ? 4 : 2;
+      part.dY = (const char*)in.dY + r0 * in.lddy * es;
+      part.Z = in.Z ? (const char*)in.Z + r0 * in.ldz * es : nullptr;
+      const dim3 grid((unsigned)((kp / 8 + 255) / 256), (unsigned)rows);
+      if (f32) dz_kernel<3><<<grid, 256, 0, st>>>(part, w.d_out, kp, dz + r0 * kp);
+      else dz_kernel<1><<<grid, 256, 0, st>>>(part, w.d_out, kp, dz + r0 * kp);
+      count_launch();
+      e = cudaGetLastError();
+      if (e != cudaSuccess) return e;
+    }
+    e = encode_map_3d(&map, dz, kp, in.n, f32 ? 3 : 1, kp, kp * in.n, 64, 2 * nh);
+  }
+  if (e != cudaSuccess) return e;
+  p.ck = 1;
+  while (p.ck < 8 && p.itiles * p.ttiles * p.ck * 2 <= sms && p.steps >= 8 * p.ck) p.ck *= 2;
+  switch (cw) {
+    case 2: return launch_nh<2>(map, p, nh, f32, sms, st);
+    case 3: return launch_nh<3>(map, p, nh, f32, sms, st);
+    case 4: return launch_nh<4>(map, p, nh, f32, sms, st);
+  }
+  return launch_nh<8>(map, p, nh, f32, sms, st);
+}
+
+}  // namespace cdq

@@ -15,9 +15,8 @@
 //   * per block the first accumulator's instructions, then the second's: while one is multiplied into, the other's group goes through the scales;
 //   * warp 0 TMA, warp 1 MMA and TMEM owner, warps 4-7 codes, warps 8-11 and 12-15 the two accumulators: acc = fma(a, D, fma(b', S, acc)) in packed fp32;
 //   * persistent blocks over the tiles; few tiles: a cluster of CK blocks shares the inputs of one and adds its sums over the cluster's shared memory.
-// A group longer than 2048 inputs is cut: the tensor core's accumulation truncates, and its error grows with the steps behind a sum.
+// A long group is cut (flush_blocks).
 // Every wait is bounded, see async_copy.cuh.
-#include <cooperative_groups.h>
 #include <cuda.h>
 
 #include "async_copy.cuh"
@@ -27,9 +26,7 @@
 namespace cdq {
 namespace {
 
-namespace cg = cooperative_groups;
-
-constexpr int BJ = 128, KB = 128, FLUSH = 16;   // columns per tile, inputs per block, blocks behind one accumulator
+constexpr int BJ = 128, KB = 128;   // columns per tile, inputs per block
 constexpr uint32_t SPIN = 1u << 24;
 constexpr int THREADS = 512;
 constexpr int A_COLS = KB / 2, A_STAGES = 4;    // TMEM columns of one block of codes
@@ -41,6 +38,10 @@ template <int NH, int TERMS> struct Shape {
   static constexpr size_t RAW = 1024 + (size_t)STAGES * X_BYTES + STAGE_OUT + 512;
   static constexpr size_t SMEM = RAW < 120 * 1024 ? 120 * 1024 : RAW;   // one block per SM: it takes all of TMEM
 };
+
+// Blocks behind one accumulator.  The tensor core's accumulation truncates, 2^-24 of the sum at every instruction of 16 inputs and term: 2048 inputs cost
+// a bf16 result nothing that shows, fp32 results take 512 (three terms 256).  The walk over a block's inputs is the same for all roles.
+__host__ __device__ constexpr int flush_blocks(int terms, bool grad) { return terms > 1 ? 2 : grad ? 4 : 16; }
 
 struct Params {
   PackedView w;
@@ -54,7 +55,7 @@ struct Params {
 };
 
 // The walk over inputs that the MMA issuer and both epilogues share: segments of a block that belong to one group; `last` where the accumulator is complete.
-struct Walk {
+template <int FLUSH> struct Walk {
   int ib, ib1, k, kend, g, t, blocks;
   bool first;
   __device__ Walk(const PackedView& w, int a, int b)
@@ -77,19 +78,17 @@ struct Walk {
   }
 };
 
-// code pairs of one column, natural order of inputs, into TMEM: 32 columns = two chunks of 32 inputs
+// code pairs of one column, natural order of inputs, into TMEM: 16 columns per chunk of 32 inputs
 template <int CW>
 __device__ __forceinline__ void store_codes(uint32_t taddr, const uint32_t (&w)[4][Piece<CW>::WORDS], const Codec<CW>& codec) {
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    uint32_t r[32];
+  for (int c = 0; c < 4; ++c) {
+    uint32_t r[16];
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int p = 0; p < 4; ++p) r[16 * c + 4 * q + p] = dequant_pair<CW>(w[q], 4 * (2 * half + c) + p, codec);
-    tmem_st32(taddr + 32 * half, r);
+      for (int p = 0; p < 4; ++p) r[4 * q + p] = dequant_pair<CW>(w[q], 4 * c + p, codec);
+    tmem_st16(taddr + 16 * c, r);
   }
 }
 
@@ -97,7 +96,7 @@ template <int CW, int NH, int TERMS, bool GRAD>
 __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ Params p) {
   extern __shared__ unsigned char smem_raw[];
   using Sh = Shape<NH, TERMS>;
-  constexpr int STAGES = Sh::STAGES;
+  constexpr int STAGES = Sh::STAGES, FLUSH = flush_blocks(TERMS, GRAD);
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t xring = (raw + 1023u) & ~1023u;
   unsigned char* base = smem_raw + (xring - raw);
@@ -131,7 +130,6 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
   const int rank = p.ck == 1 ? 0 : blockIdx.x % p.ck;
   const int ib0 = p.ck == 1 ? 0 : w.nib * rank / p.ck, ib1 = p.ck == 1 ? w.nib : w.nib * (rank + 1) / p.ck;
   const int tiles = p.jtiles * p.ttiles, tile0 = blockIdx.x / p.ck, tstep = p.ck == 1 ? gridDim.x : tiles;
-  unsigned long long acc[NH / 2];   // NH rows of the thread's column, in pairs
   const int h = (warp >> 2) - 2;    // which accumulator (warps 8-15)
   const int quarter = warp & 3;
 
@@ -156,45 +154,70 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
         }
       }
       if (!ok) drain_ring(bar0, STAGES, s, ph, issued, SPIN);
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
       constexpr uint32_t IDESC = idesc_bf16(128, NH, false, false);
+      constexpr uint32_t BOX = 2 * NH * 128;   // bytes of 64 inputs of all rows
+      const bool leader = elect_one();
       int xs = 0, as = 0;
       uint32_t xph = 0, aph = 0, dph = 1;   // dph: parity of "empty" to wait for, flips with every accumulator
       bool ok = true;
       for (int t = tile0; t < tiles && ok; t += tstep) {
-        Walk wk(w, ib0, ib1);
+        Walk<FLUSH> wk(w, ib0, ib1);
         while (!wk.done() && ok) {
-          if (!mbar_wait_or_abort(afull(as), aph, abort_flag, SPIN) || !mbar_wait_or_abort(xfull(xs), xph, abort_flag, SPIN)) { ok = false; break; }
+          ok = mbar_wait_or_abort(afull(as), aph, abort_flag, SPIN) && mbar_wait_or_abort(xfull(xs), xph, abort_flag, SPIN);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
           tc_fence_after();
-          const uint32_t x = xring + (uint32_t)xs * Sh::X_BYTES, a = tmem_a + as * A_COLS;
+          const uint32_t a = tmem_a + as * A_COLS;
+          const uint64_t x = desc_k_major(xring + (uint32_t)xs * Sh::X_BYTES);   // addresses count in units of 16 bytes
           bool through = false;
           while (!through) {
-            const int k0 = wk.k & (KB - 1), k1 = ((wk.seg_end() - 1) & (KB - 1)) + 1;
+            const int c0 = (wk.k & (KB - 1)) >> 5, c1 = ((wk.seg_end() - 1) & (KB - 1)) / 32 + 1;   // chunks of 32 inputs
             const bool first = wk.first, last = wk.last();
-#pragma unroll 1
+#pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
-              if (first && !mbar_wait_or_abort(dempty(hh), dph, abort_flag, SPIN)) { ok = false; break; }
-              if (first) tc_fence_after();
-              for (int m = 0; m < TERMS; ++m)
-                for (int k = k0; k < k1; k += 16) {
-                  const uint32_t b = x + (m * 2 + (k >> 6)) * (2 * NH * 128) + hh * (NH * 128) + (k & 63) * 2;
-                  mma_ts(tmem + hh * NH, a + k / 2, desc_k_major(b), IDESC, !(first && m == 0 && k == k0));
+              if (first) {
+                ok = __all_sync(0xffffffffu, ok && mbar_wait_or_abort(dempty(hh), dph, abort_flag, SPIN));
+                if (!ok) break;
+                tc_fence_after();
+              }
+              const uint32_t d = tmem + hh * NH;
+              if (leader) {
+                if (c0 == 0 && c1 == 4) {
+#pragma unroll
+                  for (int m = 0; m < TERMS; ++m)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                      mma_ts(d, a + 8 * k, x + ((m * 2 + k / 4) * BOX + hh * (NH * 128) + (k & 3) * 32) / 16, IDESC, m + k > 0 || !first);
+                } else {
+                  for (int c = c0; c < c1; ++c)
+#pragma unroll
+                    for (int m = 0; m < TERMS; ++m)
+#pragma unroll
+                      for (int k = 0; k < 2; ++k)
+                        mma_ts(d, a + 16 * c + 8 * k, x + ((m * 2 + c / 2) * BOX + hh * (NH * 128) + (c & 1) * 64 + k * 32) / 16, IDESC,
+                               !(first && c == c0 && m + k == 0));
                 }
-              if (last) mma_commit(dfull(hh));
+                if (last) mma_commit(dfull(hh));
+              }
+              __syncwarp();
             }
             if (!ok) break;
             if (last) dph ^= 1u;
             through = wk.next();
           }
-          mma_commit(xempty(xs));
-          mma_commit(aempty(as));
+          if (leader) {
+            mma_commit(xempty(xs));
+            mma_commit(aempty(as));
+          }
+          __syncwarp();
           if (++xs == STAGES) { xs = 0; xph ^= 1u; }
           if (++as == A_STAGES) { as = 0; aph ^= 1u; }
         }
       }
     }
   } else if (warp < 8) {
-    reg_dec<96>();
+    reg_dec<104>();
     constexpr int W = Piece<CW>::WORDS, AHEAD = CW == 8 ? 2 : 3;
     const Codec<CW> codec(w);
     uint32_t ring[AHEAD][4][W];
@@ -233,6 +256,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
     }
   } else {
     reg_inc<184>();
+    unsigned long long acc[NH / 2];   // NH rows of the thread's column, in pairs
     constexpr int STEP = NH < 32 ? NH : 16;
     uint32_t dph = 0;
     bool ok = true;
@@ -263,7 +287,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
         for (int i = 0; i < NH / 2; ++i) acc[i] = 0ull;
       }
       float ds = 0.f;
-      Walk wk(w, ib0, ib1);
+      Walk<FLUSH> wk(w, ib0, ib1);
       float a = __ldg(w.scale + (long long)min(wk.t, w.ng - 1) * w.d_out + j), b = __ldg(w.zero + (long long)min(wk.t, w.ng - 1) * w.d_out + j);
       while (!wk.done()) {
         if (!wk.last()) { wk.next(); continue; }
@@ -360,32 +384,15 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
         }
       }
     }
-  }
-
-  if (!GRAD && p.ck > 1) {
-    // every block of the cluster has its inputs' share of the tile: sums through shared memory, the rows shared out among the blocks
-    cg::cluster_group cluster = cg::this_cluster();
-    __syncthreads();   // all instructions that read the ring are done: both accumulators were waited for
-    float* mine = reinterpret_cast<float*>(base);   // [2 NH][128]
-    const int t = tile0;
-    if (warp >= 8) {
-#pragma unroll
-      for (int i = 0; i < NH; ++i) mine[(h * NH + i) * BJ + quarter * 32 + lane] = i & 1 ? hi2(acc[i / 2]) : lo2(acc[i / 2]);
+    if (!GRAD && p.ck > 1) {   // every block of the cluster has its share of the one tile
+      const int t = tile0;
+      cluster_sum<NH>(reinterpret_cast<float*>(base), acc, h, quarter * 32 + lane, rank, p.ck, [&](int i, int c, float s) {
+        const long long tok = (long long)(t / p.jtiles) * (2 * NH) + i, o = (long long)(t % p.jtiles) * BJ + c;
+        if (tok < p.n && o < w.d_out) write_out(p.ep, tok, o, s);
+      });
     }
-    cluster.sync();
-    if (warp >= 8) {
-      const long long tok0 = (long long)(t / p.jtiles) * (2 * NH);
-      const int jb = t % p.jtiles * BJ;
-      for (int o = (threadIdx.x - 256) + rank * 256; o < 2 * NH * BJ; o += p.ck * 256) {
-        const long long tok = tok0 + o / BJ, j = jb + o % BJ;
-        if (tok >= p.n || j >= w.d_out) continue;
-        float s = 0.f;
-        for (int r = 0; r < p.ck; ++r) s += *cluster.map_shared_rank(mine + o, r);
-        write_out(p.ep, tok, j, s);
-      }
-    }
-    cluster.sync();
   }
+  if (warp < 8 && !GRAD && p.ck > 1) cluster_sum_others();
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status, (int)kFlagWaitTimeout);

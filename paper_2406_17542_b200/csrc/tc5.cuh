@@ -31,14 +31,11 @@ template <> __device__ __forceinline__ void tmem_ld<16>(uint32_t a, uint32_t (&r
                : "r"(a)
                : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t a, const uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(a),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
-      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
-      "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(a), "r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+      "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
 
@@ -50,13 +47,20 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int m, int n, bool a_mn, bool 
 __device__ __forceinline__ uint64_t desc_k_major(uint32_t a) {
   return (uint64_t)((a & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
+// One lane of a converged warp.  The loops that issue matrix instructions run in all lanes, so that addresses stay in uniform registers, where the
+// instruction wants them; a loop inside one lane's branch moved them there one by one, 140 to 190 cycles per instruction.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
 // Left operand in TMEM.
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
@@ -83,6 +87,41 @@ __device__ __forceinline__ void drain_ring(uint32_t full0, int stages, int stage
     for (uint32_t it = 0; it < spin; ++it)
       if (mbar_try_wait(full0 + 8u * s, ph)) break;
   }
+}
+
+// Barriers that warps reach at different places of the code (the accumulators' registers end with their warps' branch).
+__device__ __forceinline__ void block_barrier(int threads) { asm volatile("bar.sync 0, %0;" ::"r"(threads) : "memory"); }
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// a float at the same place of the shared memory of the cluster's block `rank`
+__device__ __forceinline__ float cluster_load(const float* own, int rank) {
+  uint32_t a;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(own)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+// Sums of a cluster's blocks: each has its share of the K dimension of one tile, acc[] of 128 columns x NH rows per group of four warps (threads 256 to
+// 511).  Every block adds its part of the outputs up, ascending by block.  mine: [2 NH][128] floats of shared memory that nothing uses any more.
+template <int NH, class Out>
+__device__ __forceinline__ void cluster_sum(float* mine, const unsigned long long (&acc)[NH / 2], int h, int col, int rank, int ck, Out out) {
+  block_barrier(512);   // all instructions that read the ring are done: both accumulators were waited for
+#pragma unroll
+  for (int i = 0; i < NH; ++i) mine[(h * NH + i) * 128 + col] = __uint_as_float((uint32_t)(i & 1 ? acc[i / 2] >> 32 : acc[i / 2]));
+  cluster_barrier();
+#pragma unroll 1
+  for (int o = (threadIdx.x - 256) + rank * 256; o < 2 * NH * 128; o += ck * 256) {
+    float s = 0.f;
+    for (int r = 0; r < ck; ++r) s += cluster_load(mine + o, r);
+    out(o >> 7, o & 127, s);
+  }
+  cluster_barrier();   // no block's shared memory goes while another reads it
+}
+__device__ __forceinline__ void cluster_sum_others() {
+  block_barrier(512);
+  cluster_barrier();
+  cluster_barrier();
 }
 
 // ---- pairs of fp32 in one register pair ----
