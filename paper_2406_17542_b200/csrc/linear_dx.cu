@@ -22,7 +22,7 @@ namespace {
 constexpr int BI = 128, KB = 64, THREADS = 512;
 constexpr uint32_t SPIN = 1u << 24;
 constexpr int A_TERM = BI * KB * 2;             // 16 KB
-constexpr int STAGE_OUT = 8 * 32 * 32 * 4;
+constexpr int STAGE_OUT = 8 * 16 * 32 * 4;
 
 template <int NH, int TERMS> struct Shape {
   static constexpr int B_TERM = 2 * NH * KB * 2;
@@ -111,14 +111,13 @@ __global__ void __launch_bounds__(THREADS, 1) linear_dx_kernel(const __grid_cons
       bool ok = true;
       for (int t = tile0; t < tiles && ok; t += tstep)
         for (int kc = k0; kc < k1 && ok; kc += Sh::FLUSH) {
-          ok = __all_sync(0xffffffffu, mbar_wait_or_abort(dempty(buf), dph ^ 1u, abort_flag, SPIN));
+          ok = warp_wait(dempty(buf), dph ^ 1u, abort_flag, SPIN);
           if (!ok) break;
           tc_fence_after();
           const uint32_t d = tmem + buf * (2 * NH);
           const int kl = min(k1, kc + Sh::FLUSH);
           for (int k = kc; k < kl; ++k) {
-            ok = mbar_wait_or_abort(afull(s), ph, abort_flag, SPIN) && mbar_wait_or_abort(bfull(s), ph, abort_flag, SPIN);
-            ok = __all_sync(0xffffffffu, ok);
+            ok = warp_wait(afull(s), ph, abort_flag, SPIN) && warp_wait(bfull(s), ph, abort_flag, SPIN);
             if (!ok) break;
             tc_fence_after();
             const uint32_t at = ring + (uint32_t)s * Sh::BYTES;
@@ -180,8 +179,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_dx_kernel(const __grid_cons
           for (int c = 0; c < (CHUNKS ? 4 : 1); ++c) { a[v][c] = sc[v][c]; b[v][c] = ze[v][c]; }
         }
         if (k + 1 < k1) fetch(ib, k + 1);
-        ok = mbar_wait_or_abort(empty(s), ph ^ 1u, abort_flag, SPIN);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = warp_wait(empty(s), ph ^ 1u, abort_flag, SPIN);
         if (!ok) break;
         const uint32_t dst = ring + (uint32_t)s * Sh::BYTES;
 #pragma unroll
@@ -235,8 +233,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_dx_kernel(const __grid_cons
       for (int i = 0; i < NH / 2; ++i) acc[i] = 0ull;
       const unsigned long long one = pack2(1.f, 1.f);
       for (int kc = k0; kc < k1; kc += Sh::FLUSH) {
-        ok = mbar_wait_or_abort(dfull(buf), dph, abort_flag, SPIN);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = warp_wait(dfull(buf), dph, abort_flag, SPIN);
         if (!ok) break;
         tc_fence_after();
         const uint32_t td = tmem + buf * (2 * NH) + h * NH + ((uint32_t)(quarter * 32) << 16);
@@ -260,31 +257,13 @@ __global__ void __launch_bounds__(THREADS, 1) linear_dx_kernel(const __grid_cons
         if (++buf == 2) { buf = 0; dph ^= 1u; }
       }
       if (p.ck == 1 && ok) {
-        float* so = stage_out + (warp - 8) * 1024;
-        const int jl = (lane & 3) * 8;
         const bool whole = p.vec && jb + 32 <= w.d_in;
         const float none[8] = {};
-        constexpr int NB = NH < 32 ? NH : 32;
-#pragma unroll
-        for (int c = 0; c < NH / NB; ++c) {
-          if (tok0 + c * NB < p.n) {
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-              const unsigned long long x = acc[(c * NB + i) / 2];
-              so[i * 32 + (lane ^ ((i & 7) << 2))] = i & 1 ? hi2(x) : lo2(x);
-            }
-          }
-          __syncwarp();
 #pragma unroll 1
-          for (int i = lane >> 2; i < NB; i += 8) {
-            const long long tok = tok0 + c * NB + i;
-            if (tok >= p.n) break;
-            float z[8];
-            *reinterpret_cast<float4*>(z) = *reinterpret_cast<const float4*>(so + i * 32 + (jl ^ ((i & 7) << 2)));
-            *reinterpret_cast<float4*>(z + 4) = *reinterpret_cast<const float4*>(so + i * 32 + ((jl + 4) ^ ((i & 7) << 2)));
-            write_eight(p.ep, tok, jb + jl, w.d_in, whole, none, z);
-          }
-          __syncwarp();
+        for (int c = 0; c < NH / 16 && tok0 + 16 * c < p.n; ++c) {
+          unsigned long long x[8];
+          pick16(acc, c, x);
+          write_rows16(p.ep, stage_out + (warp - 8) * 512, x, tok0 + 16 * c, p.n, jb, w.d_in, whole, none);
         }
       }
     }
@@ -297,6 +276,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_dx_kernel(const __grid_cons
     }
   }
   if (warp < 8 && p.ck > 1) cluster_sum_others();
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status, (int)kFlagWaitTimeout);

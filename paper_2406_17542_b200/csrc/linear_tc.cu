@@ -30,12 +30,14 @@ constexpr int BJ = 128, KB = 128;   // columns per tile, inputs per block
 constexpr uint32_t SPIN = 1u << 24;
 constexpr int THREADS = 512;
 constexpr int A_COLS = KB / 2, A_STAGES = 4;    // TMEM columns of one block of codes
-constexpr int STAGE_OUT = 8 * 32 * 32 * 4;      // the epilogue's transposition, 32 x 32 per warp
+constexpr int S_STAGES = 4;
+constexpr int STAGE_OUT = 8 * 16 * 32 * 4;      // the epilogue's transposition, 16 x 32 per warp
 
 template <int NH, int TERMS> struct Shape {
   static constexpr int X_BYTES = TERMS * 2 * NH * KB * 2;   // one block of X
   static constexpr int STAGES = X_BYTES > 65536 ? 2 : X_BYTES > 49152 ? 3 : 4;
-  static constexpr size_t RAW = 1024 + (size_t)STAGES * X_BYTES + STAGE_OUT + 512;
+  static constexpr int S_BYTES = 2 * NH * 4;       // sums of the tile's rows over one group
+  static constexpr size_t RAW = 1024 + (size_t)STAGES * X_BYTES + STAGE_OUT + S_STAGES * S_BYTES + 512;
   static constexpr size_t SMEM = RAW < 120 * 1024 ? 120 * 1024 : RAW;   // one block per SM: it takes all of TMEM
 };
 
@@ -55,19 +57,21 @@ struct Params {
 };
 
 // The walk over inputs that the MMA issuer and both epilogues share: segments of a block that belong to one group; `last` where the accumulator is complete.
-template <int FLUSH> struct Walk {
+template <int FLUSH, bool CHUNKS> struct Walk;
+
+// Groups that end inside blocks: segments [k, seg_end) of a block that belong to one group; `last` where the accumulator is complete.
+template <int FLUSH> struct Walk<FLUSH, true> {
   int ib, ib1, k, kend, g, t, blocks;
   bool first;
-  __device__ Walk(const PackedView& w, int a, int b)
-      : ib(a), ib1(b), k(a * KB), kend(w.ng == 1 ? w.nib * KB : (int)w.d_in), g(w.ng == 1 ? w.nib * KB : w.g), t(a * KB / g), blocks(0), first(true) {}
-  // the segment at hand: [k, seg_end)
+  __device__ Walk(const PackedView& w, int a, int b) : ib(a), ib1(b), k(a * KB), kend((int)w.d_in), g(w.g), t(a * KB / w.g), blocks(0), first(true) {}
   __device__ int block_end() const { return min((ib + 1) * KB, kend); }
   __device__ int seg_end() const { return min(block_end(), (t + 1) * g); }
+  __device__ int chunk0() const { return (k & (KB - 1)) >> 5; }                         // the segment's chunks of 32 inputs within the block
+  __device__ int chunk1() const { return ((seg_end() - 1) & (KB - 1)) / 32 + 1; }
   __device__ bool group_ends() const { return seg_end() == (t + 1) * g; }
   __device__ bool last() const { return group_ends() || (seg_end() == block_end() && (ib + 1 == ib1 || (blocks & (FLUSH - 1)) == FLUSH - 1)); }
   __device__ bool done() const { return ib >= ib1; }
-  // returns true when the block is through
-  __device__ bool next() {
+  __device__ bool next() {   // true when the block is through
     const int e = seg_end();
     const bool b = e == block_end();
     first = last();
@@ -75,6 +79,29 @@ template <int FLUSH> struct Walk {
     k = e;
     if (b) { ++ib; ++blocks; }
     return b;
+  }
+};
+
+// Whole blocks: a few counters.  (The issuer of the matrix instructions goes through this once per block among fifteen other warps: the general walk cost
+// it 700 to 1500 cycles there, more than the instructions take.)
+template <int FLUSH> struct Walk<FLUSH, false> {
+  int left, t, group_left, per_group, flush_left;
+  bool first;
+  __device__ Walk(const PackedView& w, int a, int b) : left(b - a), per_group(w.ng == 1 ? w.nib : w.g / KB), flush_left(FLUSH), first(true) {
+    t = a / per_group;
+    group_left = per_group - (a - t * per_group);
+  }
+  __device__ static constexpr int chunk0() { return 0; }
+  __device__ static constexpr int chunk1() { return 4; }
+  __device__ bool group_ends() const { return group_left == 1; }
+  __device__ bool last() const { return group_left == 1 || left == 1 || flush_left == 1; }
+  __device__ bool done() const { return left == 0; }
+  __device__ bool next() {
+    first = last();
+    flush_left = first ? FLUSH : flush_left - 1;
+    if (--group_left == 0) { ++t; group_left = per_group; }
+    --left;
+    return true;
   }
 };
 
@@ -92,7 +119,7 @@ __device__ __forceinline__ void store_codes(uint32_t taddr, const uint32_t (&w)[
   }
 }
 
-template <int CW, int NH, int TERMS, bool GRAD>
+template <int CW, int NH, int TERMS, bool GRAD, bool CHUNKS>
 __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ Params p) {
   extern __shared__ unsigned char smem_raw[];
   using Sh = Shape<NH, TERMS>;
@@ -101,7 +128,8 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
   const uint32_t xring = (raw + 1023u) & ~1023u;
   unsigned char* base = smem_raw + (xring - raw);
   float* stage_out = reinterpret_cast<float*>(base + (size_t)STAGES * Sh::X_BYTES);
-  unsigned char* ctrl = base + (size_t)STAGES * Sh::X_BYTES + STAGE_OUT;
+  float* sring = stage_out + STAGE_OUT / 4;
+  unsigned char* ctrl = base + (size_t)STAGES * Sh::X_BYTES + STAGE_OUT + S_STAGES * Sh::S_BYTES;
   const uint32_t bar0 = smem_u32(ctrl);
   auto xfull = [&](int s) { return bar0 + 8u * s; };
   auto xempty = [&](int s) { return bar0 + 8u * (4 + s); };
@@ -109,12 +137,15 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
   auto aempty = [&](int s) { return bar0 + 8u * (12 + s); };
   auto dfull = [&](int h) { return bar0 + 8u * (16 + h); };
   auto dempty = [&](int h) { return bar0 + 8u * (18 + h); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl + 192);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl + 200);
+  auto sfull = [&](int s) { return bar0 + 8u * (20 + s); };
+  auto sempty = [&](int s) { return bar0 + 8u * (24 + s); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl + 240);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl + 248);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(xfull(s), 1); mbar_init(xempty(s), 1); }
     for (int s = 0; s < A_STAGES; ++s) { mbar_init(afull(s), 4); mbar_init(aempty(s), 1); }
+    for (int s = 0; s < S_STAGES; ++s) { mbar_init(sfull(s), 1); mbar_init(sempty(s), 8); }
     for (int h = 0; h < 2; ++h) { mbar_init(dfull(h), 1); mbar_init(dempty(h), 4); }
     *abort_flag = 0;
     mbar_fence_init();
@@ -154,6 +185,22 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
         }
       }
       if (!ok) drain_ring(bar0, STAGES, s, ph, issued, SPIN);
+    } else if (warp == 2 && lane == 0) {   // the sums S of a group, one copy for every group that ends
+      int s = 0, issued = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int t = tile0; t < tiles && ok; t += tstep) {
+        const float* S = p.S + (long long)(t / p.jtiles) * (2 * NH);
+        for (Walk<FLUSH, CHUNKS> wk(w, ib0, ib1); !wk.done() && ok; wk.next()) {
+          if (!wk.group_ends()) continue;
+          if (!mbar_wait_or_abort(sempty(s), ph ^ 1u, abort_flag, SPIN)) { ok = false; break; }
+          mbar_expect_tx(sfull(s), Sh::S_BYTES);
+          bulk_load(smem_u32(sring + s * (2 * NH)), S + wk.t * p.ldS, Sh::S_BYTES, sfull(s));
+          ++issued;
+          if (++s == S_STAGES) { s = 0; ph ^= 1u; }
+        }
+      }
+      if (!ok) drain_ring(sfull(0), S_STAGES, s, ph, issued, SPIN);
     } else if (warp == 1) {
       constexpr uint32_t IDESC = idesc_bf16(128, NH, false, false);
       constexpr uint32_t BOX = 2 * NH * 128;   // bytes of 64 inputs of all rows
@@ -162,22 +209,21 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
       uint32_t xph = 0, aph = 0, dph = 1;   // dph: parity of "empty" to wait for, flips with every accumulator
       bool ok = true;
       for (int t = tile0; t < tiles && ok; t += tstep) {
-        Walk<FLUSH> wk(w, ib0, ib1);
+        Walk<FLUSH, CHUNKS> wk(w, ib0, ib1);
         while (!wk.done() && ok) {
-          ok = mbar_wait_or_abort(afull(as), aph, abort_flag, SPIN) && mbar_wait_or_abort(xfull(xs), xph, abort_flag, SPIN);
-          ok = __all_sync(0xffffffffu, ok);
+          ok = warp_wait(afull(as), aph, abort_flag, SPIN) && warp_wait(xfull(xs), xph, abort_flag, SPIN);
           if (!ok) break;
           tc_fence_after();
           const uint32_t a = tmem_a + as * A_COLS;
           const uint64_t x = desc_k_major(xring + (uint32_t)xs * Sh::X_BYTES);   // addresses count in units of 16 bytes
           bool through = false;
           while (!through) {
-            const int c0 = (wk.k & (KB - 1)) >> 5, c1 = ((wk.seg_end() - 1) & (KB - 1)) / 32 + 1;   // chunks of 32 inputs
+            const int c0 = wk.chunk0(), c1 = wk.chunk1();
             const bool first = wk.first, last = wk.last();
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
               if (first) {
-                ok = __all_sync(0xffffffffu, ok && mbar_wait_or_abort(dempty(hh), dph, abort_flag, SPIN));
+                ok = ok && warp_wait(dempty(hh), dph, abort_flag, SPIN);
                 if (!ok) break;
                 tc_fence_after();
               }
@@ -240,8 +286,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
         for (int d = 0; d < AHEAD; ++d) {
           const int ib = b0 + d;
           if (ib >= ib1 || !ok) break;
-          ok = mbar_wait_or_abort(aempty(as), aph ^ 1u, abort_flag, SPIN);
-          ok = __all_sync(0xffffffffu, ok);
+          ok = warp_wait(aempty(as), aph ^ 1u, abort_flag, SPIN);
           if (!ok) break;
           tc_fence_after();
           store_codes<CW>(tmem_a + as * A_COLS + ((uint32_t)(quarter * 32) << 16), ring[d], codec);
@@ -258,14 +303,14 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
     reg_inc<184>();
     unsigned long long acc[NH / 2];   // NH rows of the thread's column, in pairs
     constexpr int STEP = NH < 32 ? NH : 16;
-    uint32_t dph = 0;
+    uint32_t dph = 0, sph = 0;
+    int ss = 0;
     bool ok = true;
     const float zf = (float)w.z;
     const uint32_t td = tmem + h * NH + ((uint32_t)(quarter * 32) << 16);
     for (int t = tile0; t < tiles && ok; t += tstep) {
       const int jb = t % p.jtiles * BJ + quarter * 32;
       const long long j = min((long long)jb + lane, w.d_out - 1), tok0 = (long long)(t / p.jtiles) * (2 * NH) + h * NH;
-      const float* S = p.S + tok0;
       if (GRAD) {
 #pragma unroll
         for (int i = 0; i < NH; i += 2) {
@@ -287,7 +332,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
         for (int i = 0; i < NH / 2; ++i) acc[i] = 0ull;
       }
       float ds = 0.f;
-      Walk<FLUSH> wk(w, ib0, ib1);
+      Walk<FLUSH, CHUNKS> wk(w, ib0, ib1);
       float a = __ldg(w.scale + (long long)min(wk.t, w.ng - 1) * w.d_out + j), b = __ldg(w.zero + (long long)min(wk.t, w.ng - 1) * w.d_out + j);
       while (!wk.done()) {
         if (!wk.last()) { wk.next(); continue; }
@@ -299,11 +344,10 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
           a1 = __ldg(w.scale + (long long)wk.t * w.d_out + j);
           b1 = __ldg(w.zero + (long long)wk.t * w.d_out + j);
         }
-        const float4* Sg = reinterpret_cast<const float4*>(S + g * p.ldS);
+        const float4* Sg = reinterpret_cast<const float4*>(sring + ss * (2 * NH) + h * NH);
         const unsigned long long a2 = pack2(a, a), b2 = ends ? pack2(fmaf(zf, a, b), fmaf(zf, a, b)) : 0ull;
         unsigned long long s2 = 0ull, z2 = 0ull;
-        ok = mbar_wait_or_abort(dfull(h), dph, abort_flag, SPIN);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = warp_wait(dfull(h), dph, abort_flag, SPIN) && (!ends || warp_wait(sfull(ss), sph, abort_flag, SPIN));
         if (!ok) break;
         dph ^= 1u;
         tc_fence_after();
@@ -312,10 +356,9 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
 #pragma unroll
         for (int c = 0; c < NH / STEP; ++c) {
           float4 s[STEP / 4];
-          if (!GRAD || ends) {
+          // (without the group's end b2 is zero, but what lies there need not be a number)
 #pragma unroll
-            for (int v = 0; v < STEP / 4; ++v) s[v] = __ldg(Sg + c * (STEP / 4) + v);
-          }
+          for (int v = 0; v < STEP / 4; ++v) s[v] = ends ? Sg[c * (STEP / 4) + v] : make_float4(0.f, 0.f, 0.f, 0.f);
           tmem_wait_ld();
           if (c + 1 < NH / STEP) tmem_ld<STEP>(td + (c + 1) * STEP, d[(c + 1) & 1]);
           else {
@@ -338,6 +381,11 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
           }
         }
         a = a1; b = b1;
+        if (ends) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(sempty(ss));
+          if (++ss == S_STAGES) { ss = 0; sph ^= 1u; }
+        }
         if (GRAD) {
           ds += lo2(s2) + hi2(s2);
           if (ends) {
@@ -353,34 +401,18 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
         }
       }
       if (!GRAD && p.ck == 1 && ok) {
-        // ---- bias, activation, residual: 32 rows at a time turned round in shared memory, then 8 columns of a row per lane ----
-        float* so = stage_out + (warp - 8) * 1024;
-        const int jl = (lane & 3) * 8;
         const bool whole = p.vec && jb + 32 <= w.d_out;
         float bias[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) bias[e] = p.ep.bias && jb + jl + e < w.d_out ? p.ep.bias[jb + jl + e] : 0.f;
-        constexpr int NB = NH < 32 ? NH : 32;
-#pragma unroll
-        for (int c = 0; c < NH / NB; ++c) {
-          if (tok0 + c * NB < p.n) {
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-              const unsigned long long x = acc[(c * NB + i) / 2];
-              so[i * 32 + (lane ^ ((i & 7) << 2))] = i & 1 ? hi2(x) : lo2(x);
-            }
-          }
-          __syncwarp();
+        for (int e = 0; e < 8; ++e) {
+          const long long jl = jb + (lane & 3) * 8 + e;
+          bias[e] = p.ep.bias && jl < w.d_out ? p.ep.bias[jl] : 0.f;
+        }
 #pragma unroll 1
-          for (int i = lane >> 2; i < NB; i += 8) {
-            const long long tok = tok0 + c * NB + i;
-            if (tok >= p.n) break;
-            float z[8];
-            *reinterpret_cast<float4*>(z) = *reinterpret_cast<const float4*>(so + i * 32 + (jl ^ ((i & 7) << 2)));
-            *reinterpret_cast<float4*>(z + 4) = *reinterpret_cast<const float4*>(so + i * 32 + ((jl + 4) ^ ((i & 7) << 2)));
-            write_eight(p.ep, tok, jb + jl, w.d_out, whole, bias, z);
-          }
-          __syncwarp();
+        for (int c = 0; c < NH / 16 && tok0 + 16 * c < p.n; ++c) {
+          unsigned long long x[8];
+          pick16(acc, c, x);
+          write_rows16(p.ep, stage_out + (warp - 8) * 512, x, tok0 + 16 * c, p.n, jb, w.d_out, whole, bias);
         }
       }
     }
@@ -393,6 +425,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
     }
   }
   if (warp < 8 && !GRAD && p.ck > 1) cluster_sum_others();
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status, (int)kFlagWaitTimeout);
@@ -497,7 +530,7 @@ Ws layout(const PackedView& w, cdq_dtype xt, long long n, bool copy, long long s
 
 template <int CW, int NH, int TERMS, bool GRAD>
 cudaError_t launch(const CUtensorMap& map, const Params& p, int sms, cudaStream_t st) {
-  auto kern = linear_tc_kernel<CW, NH, TERMS, GRAD>;
+  auto kern = p.w.ng > 1 && p.w.g % KB ? linear_tc_kernel<CW, NH, TERMS, GRAD, true> : linear_tc_kernel<CW, NH, TERMS, GRAD, false>;
   constexpr size_t bytes = Shape<NH, TERMS>::SMEM;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   if (e != cudaSuccess) return e;

@@ -147,30 +147,30 @@ __device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uin
 }
 
 // ---- activations -------------------------------------------------------------------------------------------------------------------------
+// z / (1 + 2^(z (k1 + k3 z^2))): SiLU with k1 = -log2(e), k3 = 0; GELU by tanh, 0.5 (1 + tanh u) = 1 / (1 + e^-2u) with u = sqrt(2 / pi) (z + 0.044715 z^3).
+__device__ __forceinline__ float sigmoid_of(float z, float k1, float k3) {
+  float e, r;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(z * fmaf(k3, z * z, k1)));
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
+}
+constexpr float kSiluK1 = -1.44269504f, kTanhK1 = -2.30220818f, kTanhK3 = -0.10294324f;
 __device__ __forceinline__ float act_of(float z, int act) {
-  switch (act) {
-    case CDQ_ACT_RELU: return z < 0.f ? 0.f : z;   // a NaN stays
-    case CDQ_ACT_SILU: return __fdividef(z, 1.f + __expf(-z));
-    case CDQ_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678f));
-    case CDQ_ACT_GELU_TANH: {
-      // 0.5 (1 + tanh u) = 1 / (1 + exp(-2 u))
-      const float u = 0.79788456f * (z + 0.044715f * z * z * z);
-      return __fdividef(z, 1.f + __expf(-2.f * u));
-    }
-  }
-  return z;
+  if (act == CDQ_ACT_NONE) return z;
+  if (act == CDQ_ACT_RELU) return z < 0.f ? 0.f : z;   // a NaN stays
+  if (act == CDQ_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678f));
+  return z * sigmoid_of(z, act == CDQ_ACT_SILU ? kSiluK1 : kTanhK1, act == CDQ_ACT_SILU ? 0.f : kTanhK3);
 }
 __device__ __forceinline__ float act_slope(float z, int act) {
   switch (act) {
     case CDQ_ACT_RELU: return z > 0.f ? 1.f : 0.f;
     case CDQ_ACT_SILU: {
-      const float s = __fdividef(1.f, 1.f + __expf(-z));
+      const float s = sigmoid_of(z, kSiluK1, 0.f);
       return s * (1.f + z * (1.f - s));
     }
     case CDQ_ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * __expf(-0.5f * z * z);
     case CDQ_ACT_GELU_TANH: {
-      const float u = 0.79788456f * (z + 0.044715f * z * z * z);
-      const float s = __fdividef(1.f, 1.f + __expf(-2.f * u));
+      const float s = sigmoid_of(z, kTanhK1, kTanhK3);
       return s + z * s * (1.f - s) * 2.f * 0.79788456f * (1.f + 0.134145f * z * z);
     }
   }

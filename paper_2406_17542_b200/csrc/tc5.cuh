@@ -89,10 +89,16 @@ __device__ __forceinline__ void drain_ring(uint32_t full0, int stages, int stage
   }
 }
 
-// Barriers that warps reach at different places of the code (the accumulators' registers end with their warps' branch).
-__device__ __forceinline__ void block_barrier(int threads) { asm volatile("bar.sync 0, %0;" ::"r"(threads) : "memory"); }
+// Barriers that warps reach at different places of the code (the accumulators' registers end with their warps' branch), and warps of which one lane worked
+// alone: the lanes meet first, and the barriers are those that do not take a converged warp for granted.
+__device__ __forceinline__ void block_barrier(int threads) {
+  __syncwarp();
+  asm volatile("barrier.sync 0, %0;" ::"r"(threads) : "memory");
+}
 __device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 // a float at the same place of the shared memory of the cluster's block `rank`
 __device__ __forceinline__ float cluster_load(const float* own, int rank) {
@@ -124,6 +130,11 @@ __device__ __forceinline__ void cluster_sum_others() {
   cluster_barrier();
 }
 
+// mbar_wait_or_abort for a whole warp: all lanes go on, or none.  (One lane polling for all was slower, 32 against 36 us at 61 x 14336 x 4096.)
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t spin) {
+  return __all_sync(0xffffffffu, mbar_wait_or_abort(bar, parity, abort_flag, spin));
+}
+
 // ---- pairs of fp32 in one register pair ----
 __device__ __forceinline__ unsigned long long pack2(float lo, float hi) {
   unsigned long long r;
@@ -138,64 +149,92 @@ __device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigne
   return r;
 }
 
-// Eight columns of a row: bias, activation, residual, stores of 16 bytes where `whole`.
-__device__ __forceinline__ void write_eight(const Epilogue& e, long long tok, long long j, long long d_out, bool whole, const float (&bias)[8], float (&z)[8]) {
-  if (!whole) {
+// Pairs 8 c .. 8 c + 7 of an array that lives in registers, c known at run time only: a few moves per branch.  (An epilogue written out for every
+// 16 rows is 40 KB of instructions, and sixteen warps with roles of their own share one instruction cache.)
+template <int P>
+__device__ __forceinline__ void pick16(const unsigned long long (&acc)[P], int c, unsigned long long (&x)[8]) {
 #pragma unroll
-    for (int v = 0; v < 8; ++v)
-      if (j + v < d_out) write_out(e, tok, j + v, z[v]);
+  for (int k = 0; k < P / 8; ++k)
+    if (c == k) {
+#pragma unroll
+      for (int v = 0; v < 8; ++v) x[v] = acc[8 * k + v];
+    }
+}
+// The way of a tile's 32 columns x 16 rows from registers to memory: acc of 16 rows of the lane's column, turned round through 2 KB of the warp's
+// own (`so`), so that a lane has eight columns of the rows lane / 4 and lane / 4 + 8: bias, activation, residual, stores of 16 bytes where `whole`.
+__device__ __forceinline__ void write_rows16(const Epilogue& e, float* so, const unsigned long long (&acc)[8], long long tok, long long n, long long j,
+                                             long long d_out, bool whole, const float (&bias)[8]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) so[i * 32 + (lane ^ ((i & 7) << 2))] = __uint_as_float((uint32_t)(i & 1 ? acc[i / 2] >> 32 : acc[i / 2]));
+  __syncwarp();
+  const int r = lane >> 2, jl = (lane & 3) * 8;
+  float z[2][8];
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    const float* from = so + (r + 8 * v) * 32;
+    *reinterpret_cast<float4*>(z[v]) = *reinterpret_cast<const float4*>(from + (jl ^ (r << 2)));
+    *reinterpret_cast<float4*>(z[v] + 4) = *reinterpret_cast<const float4*>(from + ((jl + 4) ^ (r << 2)));
+  }
+  __syncwarp();
+  j += jl;
+  tok += r;
+  if (!whole) {
+#pragma unroll 1
+    for (int v = 0; v < 2; ++v)
+      if (tok + 8 * v < n)
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          if (j + c < d_out) write_out(e, tok + 8 * v, j + c, v ? z[1][c] : z[0][c]);
     return;
   }
+  const bool bf = e.xt == CDQ_BF16;
   auto store = [&](void* to, long long at, const float (&x)[8]) {
-    if (e.xt == CDQ_BF16) {
-      uint32_t r[4];
+    if (bf) {
+      uint32_t u[4];
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * v], x[2 * v + 1]);
-        r[v] = *reinterpret_cast<const uint32_t*>(&b);
+      for (int c = 0; c < 4; ++c) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * c], x[2 * c + 1]);
+        u[c] = *reinterpret_cast<const uint32_t*>(&b);
       }
-      *reinterpret_cast<uint4*>((__nv_bfloat16*)to + at) = make_uint4(r[0], r[1], r[2], r[3]);
+      *reinterpret_cast<uint4*>((__nv_bfloat16*)to + at) = make_uint4(u[0], u[1], u[2], u[3]);
     } else {
       float* f = (float*)to + at;
       *reinterpret_cast<float4*>(f) = make_float4(x[0], x[1], x[2], x[3]);
       *reinterpret_cast<float4*>(f + 4) = make_float4(x[4], x[5], x[6], x[7]);
     }
   };
-  float y[8];
 #pragma unroll
-  for (int v = 0; v < 8; ++v) y[v] = z[v] += bias[v];
-  if (e.Z) store(e.Z, tok * e.ldz + j, z);
-  switch (e.act) {   // outside the loop over the columns
-    case CDQ_ACT_NONE: break;
-    case CDQ_ACT_RELU:
+  for (int v = 0; v < 2; ++v) {
+    if (tok + 8 * v >= n) break;
 #pragma unroll
-      for (int v = 0; v < 8; ++v) y[v] = act_of(z[v], CDQ_ACT_RELU);
-      break;
-    case CDQ_ACT_SILU:
+    for (int c = 0; c < 8; ++c) z[v][c] += bias[c];
+    if (e.Z) store(e.Z, (tok + 8 * v) * e.ldz + j, z[v]);
+    if (e.act == CDQ_ACT_RELU) {
 #pragma unroll
-      for (int v = 0; v < 8; ++v) y[v] = act_of(z[v], CDQ_ACT_SILU);
-      break;
-    case CDQ_ACT_GELU:
+      for (int c = 0; c < 8; ++c) z[v][c] = act_of(z[v][c], CDQ_ACT_RELU);
+    } else if (e.act == CDQ_ACT_GELU) {
 #pragma unroll
-      for (int v = 0; v < 8; ++v) y[v] = act_of(z[v], CDQ_ACT_GELU);
-      break;
-    default:
+      for (int c = 0; c < 8; ++c) z[v][c] = act_of(z[v][c], CDQ_ACT_GELU);
+    } else if (e.act != CDQ_ACT_NONE) {
+      const float k1 = e.act == CDQ_ACT_SILU ? kSiluK1 : kTanhK1, k3 = e.act == CDQ_ACT_SILU ? 0.f : kTanhK3;
 #pragma unroll
-      for (int v = 0; v < 8; ++v) y[v] = act_of(z[v], CDQ_ACT_GELU_TANH);
-  }
-  if (e.residual) {
-    if (e.xt == CDQ_BF16) {
-      const uint4 r = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)e.residual + tok * e.ldr + j);
-      const uint32_t u[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-      for (int v = 0; v < 4; ++v) { y[2 * v] += __uint_as_float(u[v] << 16); y[2 * v + 1] += __uint_as_float(u[v] & 0xffff0000u); }
-    } else {
-      const float* f = (const float*)e.residual + tok * e.ldr + j;
-#pragma unroll
-      for (int v = 0; v < 8; ++v) y[v] += f[v];
+      for (int c = 0; c < 8; ++c) z[v][c] *= sigmoid_of(z[v][c], k1, k3);
     }
+    if (e.residual) {
+      const long long at = (tok + 8 * v) * e.ldr + j;
+      if (bf) {
+        const uint4 q = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)e.residual + at);
+        const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) { z[v][2 * c] += __uint_as_float(u[c] << 16); z[v][2 * c + 1] += __uint_as_float(u[c] & 0xffff0000u); }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) z[v][c] += ((const float*)e.residual)[at + c];
+      }
+    }
+    store(e.Y, (tok + 8 * v) * e.ldy + j, z[v]);
   }
-  store(e.Y, tok * e.ldy + j, y);
 }
 
 // Tensor map of bf16 planes [z][y][x]: row stride ldx and plane stride ldz in entries; boxes of bx x by entries, 128-byte swizzle, zeros outside.
