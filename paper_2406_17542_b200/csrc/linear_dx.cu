@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_dx_kernel(const __grid_cons
   const int h = (warp >> 2) - 2, quarter = warp & 3;
 
   if (warp < 4) {
-    reg_dec<40>();
+    reg_dec<24>();
     if (warp == 0 && lane == 0) {
       int s = 0, issued = 0;
       uint32_t ph = 0;
@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_dx_kernel(const __grid_cons
         }
     }
   } else if (warp < 8) {
-    reg_dec<104>();
+    reg_dec<88>();
     // warp q of the four makes quarter q of 64 columns: lane, lane + 32
     constexpr int W = Piece<CW>::WORDS, PLACES = Codec<CW>::PLACES;
     const Codec<CW> codec(w);
@@ -220,9 +220,9 @@ __global__ void __launch_bounds__(THREADS, 1) linear_dx_kernel(const __grid_cons
       }
     }
   } else {
-    reg_inc<184>();
+    reg_inc<200>();
     unsigned long long acc[NH / 2];   // NH rows of the thread's column, in pairs
-    constexpr int STEP = 16;
+    constexpr int STEP = 8;
     int buf = 0;
     uint32_t dph = 0;
     bool ok = true;
@@ -258,13 +258,9 @@ __global__ void __launch_bounds__(THREADS, 1) linear_dx_kernel(const __grid_cons
       }
       if (p.ck == 1 && ok) {
         const bool whole = p.vec && jb + 32 <= w.d_in;
-        const float none[8] = {};
-#pragma unroll 1
-        for (int c = 0; c < NH / 16 && tok0 + 16 * c < p.n; ++c) {
-          unsigned long long x[8];
-          pick16(acc, c, x);
-          write_rows16(p.ep, stage_out + (warp - 8) * 512, x, tok0 + 16 * c, p.n, jb, w.d_in, whole, none);
-        }
+#pragma unroll
+        for (int c = 0; c < NH / 16; ++c)
+          if (tok0 + 16 * c < p.n) write_rows16(p.ep, stage_out + (warp - 8) * 512, acc, c, 0.f, tok0 + 16 * c, p.n, jb, w.d_in, whole);
       }
     }
     if (p.ck > 1) {   // every block of the cluster has its share of the one tile

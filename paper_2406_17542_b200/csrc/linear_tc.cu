@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
   const int quarter = warp & 3;
 
   if (warp < 4) {
-    reg_dec<40>();
+    reg_dec<24>();
     if (warp == 0 && lane == 0) {
       int s = 0, issued = 0;
       uint32_t ph = 0;
@@ -263,8 +263,8 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
       }
     }
   } else if (warp < 8) {
-    reg_dec<104>();
-    constexpr int W = Piece<CW>::WORDS, AHEAD = CW == 8 ? 2 : 3;
+    reg_dec<88>();
+    constexpr int W = Piece<CW>::WORDS, AHEAD = CW == 8 ? 1 : 3;
     const Codec<CW> codec(w);
     uint32_t ring[AHEAD][4][W];
     int as = 0;
@@ -300,9 +300,9 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
       }
     }
   } else {
-    reg_inc<184>();
+    reg_inc<200>();
     unsigned long long acc[NH / 2];   // NH rows of the thread's column, in pairs
-    constexpr int STEP = NH < 32 ? NH : 16;
+    constexpr int STEP = 8;
     uint32_t dph = 0, sph = 0;
     int ss = 0;
     bool ok = true;
@@ -402,18 +402,10 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
       }
       if (!GRAD && p.ck == 1 && ok) {
         const bool whole = p.vec && jb + 32 <= w.d_out;
-        float bias[8];
+        const float bias = p.ep.bias ? p.ep.bias[j] : 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const long long jl = jb + (lane & 3) * 8 + e;
-          bias[e] = p.ep.bias && jl < w.d_out ? p.ep.bias[jl] : 0.f;
-        }
-#pragma unroll 1
-        for (int c = 0; c < NH / 16 && tok0 + 16 * c < p.n; ++c) {
-          unsigned long long x[8];
-          pick16(acc, c, x);
-          write_rows16(p.ep, stage_out + (warp - 8) * 512, x, tok0 + 16 * c, p.n, jb, w.d_out, whole, bias);
-        }
+        for (int c = 0; c < NH / 16; ++c)
+          if (tok0 + 16 * c < p.n) write_rows16(p.ep, stage_out + (warp - 8) * 512, acc, c, bias, tok0 + 16 * c, p.n, jb, w.d_out, whole);
       }
     }
     if (!GRAD && p.ck > 1) {   // every block of the cluster has its share of the one tile

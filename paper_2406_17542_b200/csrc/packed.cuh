@@ -195,12 +195,14 @@ struct Epilogue {
   int act;
   cdq_dtype xt;
 };
-__device__ __forceinline__ void write_out(const Epilogue& e, long long tok, long long j, float z) {
-  if (e.bias) z += e.bias[j];
+__device__ __forceinline__ void write_biased(const Epilogue& e, long long tok, long long j, float z) {   // z with the bias in it
   if (e.Z) store_y(e.Z, e.xt, tok * e.ldz + j, z);
   float y = act_of(z, e.act);
   if (e.residual) y += load_x(e.residual, e.xt, tok * e.ldr + j);
   store_y(e.Y, e.xt, tok * e.ldy + j, y);
+}
+__device__ __forceinline__ void write_out(const Epilogue& e, long long tok, long long j, float z) {
+  write_biased(e, tok, j, e.bias ? z + e.bias[j] : z);
 }
 
 }  // namespace cdq

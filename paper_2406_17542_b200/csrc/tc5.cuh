@@ -31,6 +31,12 @@ template <> __device__ __forceinline__ void tmem_ld<16>(uint32_t a, uint32_t (&r
                : "r"(a)
                : "memory");
 }
+template <> __device__ __forceinline__ void tmem_ld<8>(uint32_t a, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(a)
+               : "memory");
+}
 __device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(a), "r"(r[0]),
@@ -149,92 +155,83 @@ __device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigne
   return r;
 }
 
-// Pairs 8 c .. 8 c + 7 of an array that lives in registers, c known at run time only: a few moves per branch.  (An epilogue written out for every
-// 16 rows is 40 KB of instructions, and sixteen warps with roles of their own share one instruction cache.)
+// The way of a tile's 32 columns x 16 rows from registers to memory: rows 16 c .. 16 c + 15 of the lane's column, c known at run time only, turned round
+// through 2 KB of the warp's own (`so`), so that a lane has eight columns of the rows lane / 4 and lane / 4 + 8; activation, residual, stores of 16
+// bytes where `whole`.  Few instructions (sixteen warps with roles of their own share one instruction cache) and few registers: a spilled accumulator
+// comes back from L2, since shared memory leaves L1 next to nothing, and cost the whole kernel half its speed.
 template <int P>
-__device__ __forceinline__ void pick16(const unsigned long long (&acc)[P], int c, unsigned long long (&x)[8]) {
+__device__ __forceinline__ void write_rows16(const Epilogue& e, float* so, const unsigned long long (&acc)[P], int c, float bias, long long tok, long long n,
+                                             long long j, long long d_out, bool whole) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int k = 0; k < P / 8; ++k)
     if (c == k) {
 #pragma unroll
-      for (int v = 0; v < 8; ++v) x[v] = acc[8 * k + v];
+      for (int i = 0; i < 16; ++i) {
+        const unsigned long long x = acc[8 * k + i / 2];
+        so[i * 32 + (lane ^ ((i & 7) << 2))] = __uint_as_float((uint32_t)(i & 1 ? x >> 32 : x)) + bias;
+      }
     }
-}
-// The way of a tile's 32 columns x 16 rows from registers to memory: acc of 16 rows of the lane's column, turned round through 2 KB of the warp's
-// own (`so`), so that a lane has eight columns of the rows lane / 4 and lane / 4 + 8: bias, activation, residual, stores of 16 bytes where `whole`.
-__device__ __forceinline__ void write_rows16(const Epilogue& e, float* so, const unsigned long long (&acc)[8], long long tok, long long n, long long j,
-                                             long long d_out, bool whole, const float (&bias)[8]) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) so[i * 32 + (lane ^ ((i & 7) << 2))] = __uint_as_float((uint32_t)(i & 1 ? acc[i / 2] >> 32 : acc[i / 2]));
   __syncwarp();
   const int r = lane >> 2, jl = (lane & 3) * 8;
-  float z[2][8];
-#pragma unroll
-  for (int v = 0; v < 2; ++v) {
-    const float* from = so + (r + 8 * v) * 32;
-    *reinterpret_cast<float4*>(z[v]) = *reinterpret_cast<const float4*>(from + (jl ^ (r << 2)));
-    *reinterpret_cast<float4*>(z[v] + 4) = *reinterpret_cast<const float4*>(from + ((jl + 4) ^ (r << 2)));
-  }
-  __syncwarp();
   j += jl;
-  tok += r;
-  if (!whole) {
-#pragma unroll 1
-    for (int v = 0; v < 2; ++v)
-      if (tok + 8 * v < n)
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-          if (j + c < d_out) write_out(e, tok + 8 * v, j + c, v ? z[1][c] : z[0][c]);
-    return;
-  }
   const bool bf = e.xt == CDQ_BF16;
-  auto store = [&](void* to, long long at, const float (&x)[8]) {
-    if (bf) {
-      uint32_t u[4];
+#pragma unroll 1
+  for (int v = 0; v < 16; v += 8) {
+    const long long t = tok + r + v;
+    if (t >= n) break;
+    float z[8];
+    const float* from = so + (r + v) * 32;
+    *reinterpret_cast<float4*>(z) = *reinterpret_cast<const float4*>(from + (jl ^ (r << 2)));
+    *reinterpret_cast<float4*>(z + 4) = *reinterpret_cast<const float4*>(from + ((jl + 4) ^ (r << 2)));
+    if (!whole) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * c], x[2 * c + 1]);
-        u[c] = *reinterpret_cast<const uint32_t*>(&b);
-      }
-      *reinterpret_cast<uint4*>((__nv_bfloat16*)to + at) = make_uint4(u[0], u[1], u[2], u[3]);
-    } else {
-      float* f = (float*)to + at;
-      *reinterpret_cast<float4*>(f) = make_float4(x[0], x[1], x[2], x[3]);
-      *reinterpret_cast<float4*>(f + 4) = make_float4(x[4], x[5], x[6], x[7]);
+      for (int x = 0; x < 8; ++x)
+        if (j + x < d_out) write_biased(e, t, j + x, z[x]);
+      continue;
     }
-  };
+    auto store = [&](void* to, long long at) {
+      if (bf) {
+        uint32_t u[4];
 #pragma unroll
-  for (int v = 0; v < 2; ++v) {
-    if (tok + 8 * v >= n) break;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) z[v][c] += bias[c];
-    if (e.Z) store(e.Z, (tok + 8 * v) * e.ldz + j, z[v]);
+        for (int x = 0; x < 4; ++x) {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(z[2 * x], z[2 * x + 1]);
+          u[x] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        *reinterpret_cast<uint4*>((__nv_bfloat16*)to + at) = make_uint4(u[0], u[1], u[2], u[3]);
+      } else {
+        float* f = (float*)to + at;
+        *reinterpret_cast<float4*>(f) = make_float4(z[0], z[1], z[2], z[3]);
+        *reinterpret_cast<float4*>(f + 4) = make_float4(z[4], z[5], z[6], z[7]);
+      }
+    };
+    if (e.Z) store(e.Z, t * e.ldz + j);
     if (e.act == CDQ_ACT_RELU) {
 #pragma unroll
-      for (int c = 0; c < 8; ++c) z[v][c] = act_of(z[v][c], CDQ_ACT_RELU);
+      for (int x = 0; x < 8; ++x) z[x] = act_of(z[x], CDQ_ACT_RELU);
     } else if (e.act == CDQ_ACT_GELU) {
 #pragma unroll
-      for (int c = 0; c < 8; ++c) z[v][c] = act_of(z[v][c], CDQ_ACT_GELU);
+      for (int x = 0; x < 8; ++x) z[x] = act_of(z[x], CDQ_ACT_GELU);
     } else if (e.act != CDQ_ACT_NONE) {
       const float k1 = e.act == CDQ_ACT_SILU ? kSiluK1 : kTanhK1, k3 = e.act == CDQ_ACT_SILU ? 0.f : kTanhK3;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) z[v][c] *= sigmoid_of(z[v][c], k1, k3);
+      for (int x = 0; x < 8; ++x) z[x] *= sigmoid_of(z[x], k1, k3);
     }
     if (e.residual) {
-      const long long at = (tok + 8 * v) * e.ldr + j;
+      const long long at = t * e.ldr + j;
       if (bf) {
         const uint4 q = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)e.residual + at);
         const uint32_t u[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) { z[v][2 * c] += __uint_as_float(u[c] << 16); z[v][2 * c + 1] += __uint_as_float(u[c] & 0xffff0000u); }
+        for (int x = 0; x < 4; ++x) { z[2 * x] += __uint_as_float(u[x] << 16); z[2 * x + 1] += __uint_as_float(u[x] & 0xffff0000u); }
       } else {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) z[v][c] += ((const float*)e.residual)[at + c];
+        for (int x = 0; x < 8; ++x) z[x] += ((const float*)e.residual)[at + x];
       }
     }
-    store(e.Y, (tok + 8 * v) * e.ldy + j, z[v]);
+    store(e.Y, t * e.ldy + j);
   }
+  __syncwarp();
 }
 
 // Tensor map of bf16 planes [z][y][x]: row stride ldx and plane stride ldz in entries; boxes of bx x by entries, 128-byte swizzle, zeros outside.
