@@ -400,6 +400,25 @@ cdq_status cdq_linear_backward(const cdq_packed_layer* layer, const void* dY, cd
                                const void* Z, long long ldz, cdq_act act, void* dX, long long lddx, float* dscale, float* dzero, float* dbias,
                                void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * A gated mixture-of-experts layer for a few tokens, its experts packed layers, in two kernels.
+ *   logits = X R;  for every token the top_k experts of the largest logits (ties: the lowest expert; a logit that is NaN counts as the lowest), their
+ *   weights the softmax over the chosen logits;  h_e = act(x Wg_e) * (x Wu_e);  y = sum over the chosen of weight * (h_e Wd_e).
+ *   gate, up  d_in = d_model, d_out = d_ff;  down  d_in = d_ff, d_out = d_model; the pointers are those of expert 0, the experts' codes lie
+ *             cdq_packed_bytes apart, their scales and zeros d_in/g * d_out apart.  One number of bits and one group size for the three.
+ *   X         [tokens, d_model] of type xt, leading dimension ldx;  R [d_model, experts] of type rt, dense.
+ *   Y         [tokens, d_model] of type xt, leading dimension ldy; must not overlap X.
+ *   ids       [tokens, top_k] int32 and weights [tokens, top_k] fp32, device, out: the chosen experts by falling weight.
+ * Arithmetic as in cdq_linear; the logits and h are fp32 (h is kept as bf16 terms, to 2^-16 for bf16 layers, exactly for fp32).  Only the chosen experts'
+ * codes are read.  Equal calls give equal bits.
+ * Limits: 1..32 tokens, 1..256 experts, top_k 1..16 and at most the experts, per-channel grids or groups that are multiples of 32
+ * (CDQ_ERR_UNSUPPORTED outside).  Other errors as for cdq_linear; CDQ_ERR_SHAPE where the three matrices do not fit together.
+ */
+size_t cdq_moe_workspace_bytes(cdq_dtype xt, long long tokens, long long top_k, long long d_ff);
+cdq_status cdq_moe(const cdq_packed_layer* gate, const cdq_packed_layer* up, const cdq_packed_layer* down, long long experts, const void* X, cdq_dtype xt,
+                   long long tokens, long long ldx, const void* R, cdq_dtype rt, long long top_k, cdq_act act, void* Y, long long ldy, int* ids,
+                   float* weights, void* ws, size_t ws_bytes, void* stream);
+
 /* Bytes of workspace `which` needs for these sizes (n: rows of X for the Hessian, steps per column for
  * CDQ_CALL_BCD_SOLVE, which covers either block size; otherwise not used). */
 size_t cdq_workspace_bytes(cdq_call which, long long n, long long d_in, long long d_out,

@@ -29,7 +29,7 @@ _ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 
 EXPORTS = ["cdq_hessian", "cdq_hessian_add_lambda", "cdq_init_rtn", "cdq_init_owc_cd", "cdq_cd_solve", "cdq_cd_solve_steps", "cdq_cd_solve_with_loss", "cdq_cd_solve_rows16", "cdq_bcd_solve", "cdq_layer_loss", "cdq_layer_loss_static",
            "cdq_workspace_bytes", "cdq_packed_bytes", "cdq_pack", "cdq_unpack", "cdq_linear", "cdq_linear_workspace_bytes",
-           "cdq_linear_backward", "cdq_linear_backward_workspace_bytes",
+           "cdq_linear_backward", "cdq_linear_backward_workspace_bytes", "cdq_moe", "cdq_moe_workspace_bytes",
            "cdq_last_device_status", "cdq_last_error_detail", "cdq_status_string", "cdq_version",
            "cdq_kernel_launches", "cdq_debug_expire_wait", "cdq_debug_set_device_status"]
 
@@ -131,6 +131,10 @@ def load():
     lib.cdq_linear.restype = lib.cdq_linear_backward.restype = ci
     lib.cdq_linear.argtypes = [lp, vp, ci, ll, ll, vp, ci, vp, ll, vp, ll, vp, ll, vp, sz, vp]
     lib.cdq_linear_backward.argtypes = [lp, vp, ci, ll, ll, vp, ll, vp, ll, ci, vp, ll, vp, vp, vp, vp, sz, vp]
+    lib.cdq_moe_workspace_bytes.restype = sz
+    lib.cdq_moe_workspace_bytes.argtypes = [ci, ll, ll, ll]
+    lib.cdq_moe.restype = ci
+    lib.cdq_moe.argtypes = [lp, lp, lp, ll, vp, ci, ll, ll, vp, ci, ll, ci, vp, ll, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -514,6 +518,50 @@ def cdq_linear_backward(dY: torch.Tensor, layer: PackedLayer, X: torch.Tensor | 
           (layer.ref, dY.data_ptr(), xt, n, lddy, ptr(X) if want_scales else None, ldx, ptr(Z) if act != "none" else None, ldz, _ACTS[act], ptr(dX), d_in,
            ptr(dscale), ptr(dzero), ptr(dbias), wptr, wbytes))
     return {"dX": dX, "dscale": dscale, "dzero": dzero, "dbias": dbias}
+
+
+class PackedExperts:
+    """The experts of cdq_moe: router [d_model, experts] (bf16 or fp32) and three stacks of packed layers, gate and up d_model -> d_ff, down back."""
+
+    __slots__ = ("router", "gate", "up", "down", "rt", "experts", "d_model", "d_ff")
+
+    def __init__(self, router: torch.Tensor, gate: PackedLayer, up: PackedLayer, down: PackedLayer):
+        E, d, f = gate.experts, gate.d_in, gate.d_out
+        if not E or up.experts != E or down.experts != E:
+            raise ValueError("gate, up and down have to be stacks of the same number of experts")
+        if (up.d_in, up.d_out) != (d, f) or (down.d_in, down.d_out) != (f, d):
+            raise ValueError("gate and up have to be d_model x d_ff, down d_ff x d_model")
+        if len({(t.bits, t.group_size, t.device) for t in (gate, up, down)}) != 1:
+            raise ValueError("gate, up and down need the same bits, group size and device")
+        if tuple(router.shape) != (d, E) or not router.is_contiguous() or router.device != gate.device:
+            raise ValueError(f"the router has to be a contiguous tensor of shape {(d, E)} on {gate.device}")
+        self.router, self.gate, self.up, self.down, self.rt = router, gate, up, down, _dtype_code(router)
+        self.experts, self.d_model, self.d_ff = E, d, f
+
+
+def cdq_moe(X: torch.Tensor, experts: PackedExperts, top_k: int, act: str = "silu", out: torch.Tensor | None = None, ws: Workspace | None = None):
+    """A whole mixture-of-experts layer for up to 32 tokens: (Y, ids [tokens, top_k] int32, weights [tokens, top_k] fp32)."""
+    if X.device != experts.gate.device:
+        raise ValueError(f"X is on {X.device}, the experts on {experts.gate.device}")
+    xt = _dtype_code(X)
+    d = experts.d_model
+    ldx = _rows_of(X, "X", None, d, X)
+    n = X.shape[0]
+    if act not in _ACTS:
+        raise ValueError(f"act is one of {', '.join(_ACTS)}")
+    if out is None:
+        Y, ldy = torch.empty((n, d), dtype=X.dtype, device=X.device), d
+    else:
+        Y, ldy = out, _rows_of(out, "out", n, d, X)
+    k = int(top_k)
+    ids = torch.empty((n, max(k, 0)), dtype=torch.int32, device=X.device)
+    weights = torch.empty((n, max(k, 0)), dtype=torch.float32, device=X.device)
+    lib = load()
+    keep, wptr, wbytes = _scratch(lib.cdq_moe_workspace_bytes(xt, n, k, experts.d_ff), X.device, ws)
+    _call(lib.cdq_moe, "cdq_moe", experts.gate.index,
+          (experts.gate.ref, experts.up.ref, experts.down.ref, experts.experts, X.data_ptr(), xt, n, ldx, experts.router.data_ptr(), experts.rt, k, _ACTS[act],
+           Y.data_ptr(), ldy, ids.data_ptr(), weights.data_ptr(), wptr, wbytes))
+    return Y, ids, weights
 
 
 STATIC_SCRATCH_BYTES = 20 * 1024 * 1024

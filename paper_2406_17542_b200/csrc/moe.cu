@@ -1,0 +1,532 @@
+// A gated mixture-of-experts layer for up to 32 tokens whose experts are packed layers, in two kernels:
+//
+//   moe_up    logits = x R, the top k of every token (ties: lowest expert), weights = softmax over them; for every expert with tokens
+//             h = act(x Wg) * (x Wu)
+//   moe_down  y[t] = sum over the token's experts of weight * (h Wd)
+//
+// Products as in linear_skinny.cu: bf16 matrix instructions with exact operands, fp32 sums, scales once per group.  h is kept as bf16 terms of the fp32
+// value (two for bf16 layers: 2^-16; three for fp32), so no rounding comes between the kernels.
+//
+// Bound by the bytes of the chosen experts.  A warp's codes come by bulk copies into a ring of its own that runs on across tiles, matrices and experts; the
+// rows come from L1.  The router is computed by every cluster of four blocks for itself (each a quarter of the inputs, exchanged over the
+// cluster's shared memory), which costs a microsecond and saves a launch and a pass over memory.  Everything is added in a fixed order.
+#include "async_copy.cuh"
+#include "linear.cuh"
+#include "skinny.cuh"
+#include "tc5.cuh"
+
+namespace cdq {
+namespace {
+
+constexpr int kTok = 32, kExperts = 256, kTop = 16, CL = 4, WARPS = 8;
+constexpr unsigned kWait = 1u << 30;
+
+// What moe_up leaves for moe_down.
+struct Lists {
+  int active;                       // experts with tokens
+  int expert[kExperts];             // ascending
+  int start[kExperts + 1];          // their pairs in `pair`
+  int pair[kTok * kTop];            // token * top_k + slot, ascending within an expert
+  float weight[kTok * kTop];        // by pair
+};
+
+struct Params {
+  PackedView gate, up, down;        // of expert 0
+  size_t codes_ff, codes_dm;        // bytes from one expert's codes to the next (gate and up, down)
+  const void* X;
+  const void* R;
+  __nv_bfloat16* h;                 // [terms][pairs][ffp]
+  Lists* lists;
+  void* Y;
+  int* ids;
+  float* weights;
+  int* status;
+  long long ldx, ldy, ffp;
+  cdq_dtype xt, rt;
+  int tokens, experts, top_k, act, vec;
+};
+
+__device__ __forceinline__ PackedView expert_view(PackedView v, size_t codes, int e) {
+  v.codes += codes * e;
+  v.scale += (long long)e * v.ng * v.d_out;
+  v.zero += (long long)e * v.ng * v.d_out;
+  return v;
+}
+
+// Rows of the right operand: tile t's row lane / 4, eight inputs from i on, as bf16 pairs of TERMS terms.
+template <int TERMS, bool F32>
+__device__ __forceinline__ void load_b(const void* base, long long ld, long long term, long long row, long long i, long long len, bool vec,
+                                       uint32_t (&x)[TERMS][4]) {
+  if (F32) {
+    const float* p = (const float*)base + row * ld + i;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      uint32_t a[3], b[3];
+      split3(i + 2 * v < len ? p[2 * v] : 0.f, a[0], a[1], a[2]);
+      split3(i + 2 * v + 1 < len ? p[2 * v + 1] : 0.f, b[0], b[1], b[2]);
+#pragma unroll
+      for (int m = 0; m < TERMS; ++m) x[m][v] = a[m] | b[m] << 16;
+    }
+    return;
+  }
+#pragma unroll
+  for (int m = 0; m < TERMS; ++m) {
+    const __nv_bfloat16* p = (const __nv_bfloat16*)base + m * term + row * ld + i;
+    if (vec && i + 8 <= len) {
+      const uint4 y = *reinterpret_cast<const uint4*>(p);
+      x[m][0] = y.x; x[m][1] = y.y; x[m][2] = y.z; x[m][3] = y.w;
+    } else {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const uint32_t lo = i + 2 * v < len ? __bfloat16_as_ushort(p[2 * v]) : 0, hi = i + 2 * v + 1 < len ? __bfloat16_as_ushort(p[2 * v + 1]) : 0;
+        x[m][v] = lo | hi << 16;
+      }
+    }
+  }
+}
+
+// A warp's sums over one stretch of blocks of one tile of columns.
+template <int CW, int NT, int TERMS, int GM, bool F32>
+struct Tile {
+  float acc[NT][4], P[NT][4], S[NT][4];
+  const float *scale, *zero;
+  int dj, g32, d_in;
+  float z;
+  long long d_out;
+  __device__ __forceinline__ void start(const PackedView& w, int jt) {
+    const int row = (threadIdx.x & 31) >> 2;
+    const long long j0 = min((long long)jt * 16 + row, w.d_out - 1), j1 = min((long long)jt * 16 + row + 8, w.d_out - 1);
+    scale = w.scale + j0; zero = w.zero + j0; dj = (int)(j1 - j0);
+    z = (float)w.z; g32 = w.g / 32; d_in = (int)w.d_in; d_out = w.d_out;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) acc[t][v] = P[t][v] = S[t][v] = 0.f;
+  }
+  __device__ __forceinline__ void fetch(int group, float (&s)[4]) const {
+    const long long at = group * d_out;
+    s[0] = __ldg(scale + at); s[1] = __ldg(zero + at); s[2] = __ldg(scale + at + dj); s[3] = __ldg(zero + at + dj);
+  }
+  __device__ __forceinline__ void scales(int group) {
+    float s[4];
+    fetch(group, s);
+    promote<NT>(s, z, S, P, acc);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) P[t][v] = S[t][v] = 0.f;
+  }
+  // one block of 128 inputs; rows: the lane's row of every tile of eight; n: rows in use
+  __device__ __forceinline__ void block(const unsigned char* codes, int ib, const Codec<CW>& k, const void* X, long long ld, long long term, const int (&rows)[NT],
+                                        int n, long long len, bool vec) {
+    constexpr int W = Piece<CW>::WORDS;
+    constexpr uint32_t ONES = 0x3f803f80u;
+    const int lane = threadIdx.x & 31, row = lane >> 2, q = lane & 3;
+    uint32_t w[2 * W];
+    load_piece<CW>(codes, Piece<CW>::part(row, q), w);
+    load_piece<CW>(codes, Piece<CW>::part(row + 8, q), w + W);
+    float s[4];
+    if (GM == 1) fetch(ib * 4 / g32, s);   // on its way while the block is multiplied
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      uint32_t a[4], b[4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) { a[p] = dequant_pair<CW>(w, 4 * c + p, k); b[p] = dequant_pair<CW>(w + W, 4 * c + p, k); }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if (t * 8 >= n) break;
+        uint32_t x[TERMS][4];
+        load_b<TERMS, F32>(X, ld, term, rows[t], (long long)ib * 128 + 32 * c + 8 * q, len, vec, x);
+#pragma unroll
+        for (int m = 0; m < TERMS; ++m) {
+          mma_16816(P[t], a[0], b[0], a[1], b[1], x[m][0], x[m][1]);
+          mma_16816(S[t], ONES, ONES, ONES, ONES, x[m][0], x[m][1]);
+          mma_16816(P[t], a[2], b[2], a[3], b[3], x[m][2], x[m][3]);
+          mma_16816(S[t], ONES, ONES, ONES, ONES, x[m][2], x[m][3]);
+        }
+      }
+      if (GM == 2 && ib * 128 + 32 * c < d_in) scales((ib * 4 + c) / g32);
+    }
+    if (GM == 1) {
+      promote<NT>(s, z, S, P, acc);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) P[t][v] = S[t][v] = 0.f;
+    }
+  }
+  __device__ __forceinline__ void finish() {
+    if (GM == 0) scales(0);
+  }
+};
+
+// ---- the router, in every cluster of CL blocks ----
+// part: [tokens][256] floats, partial logits by thread; logits: [tokens][experts]
+__device__ __forceinline__ void route(const Params& p, long long d_in, float* part, float* logits, Lists& L, int rank) {
+  const int E = p.experts, T = p.tokens, k = p.top_k, tid = threadIdx.x;
+  int ep = 8;
+  while (ep < E) ep *= 2;
+  const int e = tid & (ep - 1), rg = tid / ep, groups = 256 / ep;
+  const long long i0 = d_in * rank / CL, i1 = d_in * (rank + 1) / CL;
+  for (int t0 = 0; t0 < T; t0 += 8) {
+    float acc[8] = {};
+    if (e < E) {
+#pragma unroll 4
+      for (long long i = i0 + rg; i < i1; i += groups) {
+        const float r = load_x(p.R, p.rt, i * E + e);
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          if (t0 + t < T) acc[t] = fmaf(load_x(p.X, p.xt, (t0 + t) * p.ldx + i), r, acc[t]);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+      if (t0 + t < T) part[(t0 + t) * 256 + tid] = acc[t];
+  }
+  __syncthreads();
+  for (int v = tid; v < T * E; v += 256) {   // this block's share of the inputs
+    const int t = v / E, x = v - t * E;
+    float s = 0.f;
+    for (int r = 0; r < groups; ++r) s += part[t * 256 + r * ep + x];
+    logits[t * E + x] = s;
+  }
+  cluster_barrier();
+  float mine[kTok];
+#pragma unroll
+  for (int u = 0; u < kTok; ++u) {
+    const int v = tid + u * 256;
+    if (v < T * E) {
+      float s = 0.f;
+      for (int r = 0; r < CL; ++r) s += cluster_load(logits + v, r);
+      mine[u] = s;
+    }
+  }
+  cluster_barrier();   // all have read all
+#pragma unroll
+  for (int u = 0; u < kTok; ++u) {
+    const int v = tid + u * 256;
+    if (v < T * E) logits[v] = mine[u];
+  }
+  __syncthreads();
+  // top k: a warp per token; a logit that is not a number counts as the lowest
+  const int warp = tid >> 5, lane = tid & 31;
+  int* ids = reinterpret_cast<int*>(part);
+  for (int t = warp; t < T; t += WARPS) {
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int x = lane + 32 * u;
+      const float y = x < E ? logits[t * E + x] : -INFINITY;
+      v[u] = y == y ? y : -INFINITY;
+    }
+    unsigned taken = 0;
+    float best0 = 0.f, sum = 0.f, w = 0.f;
+    for (int s = 0; s < k; ++s) {
+      float b = -INFINITY;
+      int at = 1 << 20;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (lane + 32 * u < E && !(taken >> u & 1) && (v[u] > b || at == 1 << 20)) { b = v[u]; at = lane + 32 * u; }
+#pragma unroll
+      for (int d = 16; d; d >>= 1) {
+        const float ob = __shfl_xor_sync(0xffffffffu, b, d);
+        const int oa = __shfl_xor_sync(0xffffffffu, at, d);
+        if (oa != 1 << 20 && (at == 1 << 20 || ob > b || (ob == b && oa < at))) { b = ob; at = oa; }
+      }
+      if ((at & 31) == lane) taken |= 1u << (at >> 5);
+      if (s == 0) best0 = b;
+      const float x = b == best0 ? 1.f : expf(b - best0);
+      sum += x;
+      if (lane == s) { w = x; ids[t * k + s] = at; }
+    }
+    if (lane < k) L.weight[t * k + lane] = w / sum;
+  }
+  __syncthreads();
+  // pairs by expert: thread e looks for its own
+  int count = 0;
+  if (tid < E)
+    for (int v = 0; v < T * k; ++v) count += ids[v] == tid;
+  int before = count, rankin = count > 0;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int a = __shfl_up_sync(0xffffffffu, before, d), b = __shfl_up_sync(0xffffffffu, rankin, d);
+    if (lane >= d) { before += a; rankin += b; }
+  }
+  int* tot = ids + T * kTop;
+  if (lane == 31) { tot[warp] = before; tot[8 + warp] = rankin; }
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) { before += tot[w]; rankin += tot[8 + w]; }
+  if (count) {
+    int at = before - count;
+    L.expert[rankin - 1] = tid;
+    L.start[rankin - 1] = at;
+    for (int v = 0; v < T * k; ++v)
+      if (ids[v] == tid) L.pair[at++] = v;
+  }
+  if (tid == 255) { L.active = rankin; L.start[rankin] = T * k; }
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int v = tid; v < T * k; v += 256) { p.ids[v] = ids[v]; p.weights[v] = L.weight[v]; }
+}
+
+template <int CW> constexpr int kChunk = CW == 2 ? 4 : CW == 3 ? 3 : CW == 4 ? 2 : 1;
+constexpr int kStages = 4;
+
+template <int CW, int NT, int TERMS, int GM, bool F32>
+__global__ void __launch_bounds__(256, 2) moe_up_kernel(const __grid_constant__ Params p) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  constexpr int C = kChunk<CW>, BLOCK = Piece<CW>::BLOCK, BYTES = C * BLOCK;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane >> 2, q = lane & 3;
+  unsigned char* ring = smem + warp * (kStages * BYTES);
+  const uint32_t bars = smem_u32(smem + WARPS * kStages * BYTES) + warp * (kStages * 8);
+  Lists& L = *reinterpret_cast<Lists*>(smem + WARPS * kStages * (BYTES + 8));
+  float* red = reinterpret_cast<float*>(smem + WARPS * kStages * (BYTES + 8) + (sizeof(Lists) + 15) / 16 * 16);   // [2 parities][8 warps][2][16 columns][NT * 8]: the router is done with by then
+  if (lane == 0) {
+    for (int s = 0; s < kStages; ++s) mbar_init(bars + 8 * s, 1);
+    mbar_fence_init();
+  }
+  __syncwarp();
+  route(p, p.gate.d_in, red, red + p.tokens * 256, L, blockIdx.x % CL);
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int v = threadIdx.x; v < (int)(sizeof(Lists) / 4); v += 256) reinterpret_cast<int*>(p.lists)[v] = reinterpret_cast<const int*>(&L)[v];
+  const int terms_h = F32 ? 3 : 2, pairs = p.tokens * p.top_k, pad = (int)(p.ffp - p.gate.d_out);
+  for (int v = blockIdx.x * 256 + threadIdx.x; v < terms_h * pairs * pad; v += gridDim.x * 256)   // columns past d_ff are multiplied by padded codes
+    p.h[(long long)(v / pad) * p.ffp + p.gate.d_out + v % pad] = __float2bfloat16(0.f);
+
+  const int njt = p.gate.njt, nib = p.gate.nib, units = L.active * njt;
+  const int b0 = nib * warp / WARPS, b1 = nib * (warp + 1) / WARPS, cpm = (b1 - b0 + C - 1) / C;
+  const Codec<CW> codec(p.gate);
+  // the warp's chunks: for every unit of the block, gate then up, its share of the inputs
+  int pu = blockIdx.x, pm = 0, pc = 0, ps = 0;   // what is asked for next
+  auto request = [&]() {
+    if (cpm == 0 || pu >= units) return;
+    const int a = pu / njt, jt = pu - a * njt, first = b0 + pc * C, bytes = min(C, b1 - first) * BLOCK;
+    const unsigned char* codes = (pm ? p.up.codes : p.gate.codes) + p.codes_ff * L.expert[a] + ((long long)jt * nib + first) * BLOCK;
+    if (lane == 0) {
+      mbar_expect_tx(bars + 8 * ps, bytes);
+      bulk_load(smem_u32(ring + ps * BYTES), codes, bytes, bars + 8 * ps);
+    }
+    if (++ps == kStages) ps = 0;
+    if (++pc == cpm) { pc = 0; if (++pm == 2) { pm = 0; pu += gridDim.x; } }
+  };
+  for (int s = 0; s < kStages; ++s) request();
+  int stage = 0, parity = 0;
+  uint32_t phase = 0;
+  bool ok = true;
+  Tile<CW, NT, TERMS, GM, F32> tile;
+  for (int u = blockIdx.x; u < units; u += gridDim.x, parity ^= 1) {
+    const int a = u / njt, jt = u - a * njt, e = L.expert[a], s0 = L.start[a], n = L.start[a + 1] - s0;
+    int rows[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) rows[t] = L.pair[s0 + min(t * 8 + row, n - 1)] / p.top_k;
+    float* out = red + ((parity * WARPS + warp) * 2) * (16 * NT * 8);
+#pragma unroll 1
+    for (int m = 0; m < 2; ++m) {
+      tile.start(expert_view(m ? p.up : p.gate, p.codes_ff, e), jt);
+      for (int c = 0; c < cpm; ++c) {
+        ok = mbar_wait_clock32(bars + 8 * stage, phase, ok ? kWait : 1u) && ok;
+        const int first = b0 + c * C, have = min(C, b1 - first);
+        for (int b = 0; b < have; ++b)
+          tile.block(ring + stage * BYTES + b * BLOCK, first + b, codec, p.X, p.ldx, 0, rows, n, p.gate.d_in, p.vec);
+        __syncwarp();
+        request();
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      }
+      if (cpm) tile.finish();
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) out[m * (16 * NT * 8) + (t * 8 + 2 * q + (v & 1)) * 16 + row + 8 * (v >> 1)] = tile.acc[t][v];
+    }
+    __syncthreads();
+    for (int o = threadIdx.x; o < n * 16; o += 256) {
+      const long long j = (long long)jt * 16 + (o & 15);
+      float g = 0.f, v = 0.f;
+      for (int w = 0; w < WARPS; ++w) {
+        const float* from = red + ((parity * WARPS + w) * 2) * (16 * NT * 8) + o;
+        g += from[0];
+        v += from[16 * NT * 8];
+      }
+      if (j >= p.gate.d_out) continue;
+      uint32_t t3[3];
+      split3(act_of(g, p.act) * v, t3[0], t3[1], t3[2]);
+      const long long at = (long long)L.pair[s0 + (o >> 4)] * p.ffp + j;
+      for (int m = 0; m < terms_h; ++m) p.h[(long long)m * pairs * p.ffp + at] = __ushort_as_bfloat16((unsigned short)t3[m]);
+    }
+  }
+  if (!ok && lane == 0) atomicCAS(p.status, (int)kFlagOk, (int)kFlagWaitTimeout);
+}
+
+template <int CW, int NT, int TERMS, int GM>
+__global__ void __launch_bounds__(256, 2) moe_down_kernel(const __grid_constant__ Params p, int ck) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  constexpr int C = kChunk<CW>, BLOCK = Piece<CW>::BLOCK, BYTES = C * BLOCK;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane >> 2, q = lane & 3;
+  unsigned char* ring = smem + warp * (kStages * BYTES);
+  const uint32_t bars = smem_u32(smem + WARPS * kStages * BYTES) + warp * (kStages * 8);
+  Lists& L = *reinterpret_cast<Lists*>(smem + WARPS * kStages * (BYTES + 8));
+  float* y = reinterpret_cast<float*>(smem + WARPS * kStages * (BYTES + 8) + (sizeof(Lists) + 15) / 16 * 16);   // [8 warps][tokens][16]
+  const int rank = blockIdx.x % ck, jt = blockIdx.x / ck, T = p.tokens;
+  if (lane == 0) {
+    for (int s = 0; s < kStages; ++s) mbar_init(bars + 8 * s, 1);
+    mbar_fence_init();
+  }
+  for (int v = threadIdx.x; v < (int)(sizeof(Lists) / 4); v += 256) reinterpret_cast<int*>(&L)[v] = reinterpret_cast<const int*>(p.lists)[v];
+  float* mine = y + warp * (T * 16);
+  for (int v = lane; v < T * 16; v += 32) mine[v] = 0.f;
+  __syncthreads();
+  // all blocks of the active experts in a row, shared out among the warps of the cluster
+  const int nib = p.down.nib, total = L.active * nib, W = WARPS * ck, wi = rank * WARPS + warp;
+  const int f0 = (int)((long long)total * wi / W), f1 = (int)((long long)total * (wi + 1) / W);
+  auto chunk = [&](int f) { return min(min(C, f1 - f), nib - f % nib); };
+  int pf = f0, ps = 0;
+  auto request = [&]() {
+    if (pf >= f1) return;
+    const int a = pf / nib, n = chunk(pf);
+    if (lane == 0) {
+      const unsigned char* codes = p.down.codes + p.codes_dm * L.expert[a] + ((long long)jt * nib + (pf - a * nib)) * BLOCK;
+      mbar_expect_tx(bars + 8 * ps, n * BLOCK);
+      bulk_load(smem_u32(ring + ps * BYTES), codes, n * BLOCK, bars + 8 * ps);
+    }
+    pf += n;
+    if (++ps == kStages) ps = 0;
+  };
+  for (int s = 0; s < kStages; ++s) request();
+  const Codec<CW> codec(p.down);
+  const long long term = (long long)T * p.top_k * p.ffp;
+  int stage = 0;
+  uint32_t phase = 0;
+  bool ok = true;
+  Tile<CW, NT, TERMS, GM, false> tile;
+  for (int f = f0; f < f1;) {
+    const int a = f / nib, s0 = L.start[a], n = L.start[a + 1] - s0, fe = min(f1, (a + 1) * nib);
+    int rows[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) rows[t] = L.pair[s0 + min(t * 8 + row, n - 1)];
+    tile.start(expert_view(p.down, p.codes_dm, L.expert[a]), jt);
+    while (f < fe) {
+      const int have = chunk(f);
+      ok = mbar_wait_clock32(bars + 8 * stage, phase, ok ? kWait : 1u) && ok;
+      for (int b = 0; b < have; ++b) tile.block(ring + stage * BYTES + b * BLOCK, f + b - a * nib, codec, p.h, p.ffp, term, rows, n, p.ffp, true);
+      __syncwarp();
+      request();
+      if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      f += have;
+    }
+    tile.finish();
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int slot = t * 8 + 2 * q + (v & 1);
+        if (slot < n) {
+          const int pair = L.pair[s0 + slot];
+          float& to = mine[pair / p.top_k * 16 + row + 8 * (v >> 1)];   // an expert has a token once: no two lanes meet
+          to = fmaf(L.weight[pair], tile.acc[t][v], to);
+        }
+      }
+    __syncwarp();
+  }
+  if (!ok && lane == 0) atomicCAS(p.status, (int)kFlagOk, (int)kFlagWaitTimeout);
+  __syncthreads();
+  for (int o = threadIdx.x; o < T * 16; o += 256) {
+    float s = y[o];
+    for (int w = 1; w < WARPS; ++w) s += y[w * (T * 16) + o];
+    y[o] = s;   // read by this thread alone so far
+  }
+  if (ck > 1) cluster_barrier();
+  for (int o = threadIdx.x + rank * 256; o < T * 16; o += 256 * ck) {
+    float s = 0.f;
+    if (ck == 1) s = y[o];
+    else
+      for (int r = 0; r < ck; ++r) s += cluster_load(y + o, r);
+    const long long j = (long long)jt * 16 + (o & 15);
+    if (j < p.down.d_out) store_y(p.Y, p.xt, (o >> 4) * p.ldy + j, s);
+  }
+  if (ck > 1) cluster_barrier();
+}
+
+template <class K>
+cudaError_t start(K kern, int blocks, int cluster, size_t bytes, cudaStream_t st, cudaLaunchConfig_t& cfg, cudaLaunchAttribute* at) {
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e != cudaSuccess) return e;
+  cfg = cudaLaunchConfig_t{};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = st;
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)cluster;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  count_launch();
+  return cudaSuccess;
+}
+
+template <int CW, int NT, int GM, bool F32>
+cudaError_t run(const Params& p, int sms, cudaStream_t st) {
+  constexpr size_t ring = WARPS * kStages * (kChunk<CW> * Piece<CW>::BLOCK + 8), lists = (sizeof(Lists) + 15) / 16 * 16;
+  constexpr size_t red = 2 * WARPS * 2 * 16 * NT * 8 * sizeof(float);
+  const size_t logits = (size_t)p.tokens * (256 + p.experts) * sizeof(float), router = logits > red ? logits : red;
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute at[1];
+  const long long most = (long long)p.gate.njt * (p.experts < p.tokens * p.top_k ? p.experts : p.tokens * p.top_k);
+  const long long wanted = (most + CL - 1) / CL * CL, full = sms * 2 / CL * CL;
+  auto up = moe_up_kernel<CW, NT, F32 ? 3 : 1, GM, F32>;
+  cudaError_t e = start(up, (int)(wanted < full ? wanted : full), CL, ring + lists + router, st, cfg, at);
+  if (e != cudaSuccess) return e;
+  e = cudaLaunchKernelEx(&cfg, up, p);
+  if (e != cudaSuccess) return e;
+  int ck = 1;
+  while (ck < 8 && (long long)p.down.njt * ck < 2 * sms) ck *= 2;
+  auto down = moe_down_kernel<CW, NT, F32 ? 3 : 2, GM>;
+  e = start(down, p.down.njt * ck, ck, ring + lists + (size_t)WARPS * p.tokens * 16 * sizeof(float), st, cfg, at);
+  if (e != cudaSuccess) return e;
+  return cudaLaunchKernelEx(&cfg, down, p, ck);
+}
+
+template <int CW, bool F32>
+cudaError_t run_gm(const Params& p, int gm, int sms, cudaStream_t st) {
+  if (p.tokens <= 8) return gm == 0 ? run<CW, 1, 0, F32>(p, sms, st) : gm == 1 ? run<CW, 1, 1, F32>(p, sms, st) : run<CW, 1, 2, F32>(p, sms, st);
+  return gm == 0 ? run<CW, 4, 0, F32>(p, sms, st) : gm == 1 ? run<CW, 4, 1, F32>(p, sms, st) : run<CW, 4, 2, F32>(p, sms, st);
+}
+
+}  // namespace
+
+size_t moe_workspace(cdq_dtype xt, int tokens, int top_k, long long d_ff) {
+  return align_up(sizeof(Lists)) + align_up((size_t)(xt == CDQ_F32 ? 3 : 2) * tokens * top_k * packed_blocks(d_ff) * 128 * 2);
+}
+
+cudaError_t launch_moe(const PackedView& gate, const PackedView& up, const PackedView& down, int bits, const void* X, cdq_dtype xt, int tokens, long long ldx,
+                       const void* R, cdq_dtype rt, int experts, int top_k, int act, void* Y, long long ldy, int* ids, float* weights, void* ws,
+                       cudaStream_t st) {
+  Params p{};
+  p.gate = gate; p.up = up; p.down = down;
+  p.codes_ff = packed_bytes_of(bits, gate.d_in, gate.d_out);
+  p.codes_dm = packed_bytes_of(bits, down.d_in, down.d_out);
+  p.X = X; p.R = R; p.Y = Y; p.ids = ids; p.weights = weights;
+  p.lists = (Lists*)ws;
+  p.h = (__nv_bfloat16*)((char*)ws + align_up(sizeof(Lists)));
+  p.ldx = ldx; p.ldy = ldy; p.ffp = packed_blocks(gate.d_out) * 128;
+  p.xt = xt; p.rt = rt; p.tokens = tokens; p.experts = experts; p.top_k = top_k; p.act = act;
+  p.vec = xt == CDQ_BF16 && ldx % 8 == 0 && aligned16(X);
+  p.status = device_status_word();
+  if (!p.status) return cudaErrorInvalidSymbol;
+  int dev = 0, sms = 0;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  const bool f32 = xt == CDQ_F32;
+  // one rule for the three matrices: the finest place where a group of any of them can end
+  const auto kind = [](const PackedView& w) { return w.ng == 1 ? 0 : w.g % 128 == 0 ? 1 : 2; };
+  const int gm = kind(gate) > kind(down) ? kind(gate) : kind(down);
+  switch (packed_width(bits)) {
+    case 2: return f32 ? run_gm<2, true>(p, gm, sms, st) : run_gm<2, false>(p, gm, sms, st);
+    case 3: return f32 ? run_gm<3, true>(p, gm, sms, st) : run_gm<3, false>(p, gm, sms, st);
+    case 4: return f32 ? run_gm<4, true>(p, gm, sms, st) : run_gm<4, false>(p, gm, sms, st);
+  }
+  return f32 ? run_gm<8, true>(p, gm, sms, st) : run_gm<8, false>(p, gm, sms, st);
+}
+
+}  // namespace cdq
