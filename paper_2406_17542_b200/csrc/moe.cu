@@ -126,7 +126,7 @@ struct Tile {
     load_piece<CW>(codes, Piece<CW>::part(row, q), w);
     load_piece<CW>(codes, Piece<CW>::part(row + 8, q), w + W);
     float s[4];
-    if (GM == 1) fetch(ib * 4 / g32, s);   // on its way while the block is multiplied
+    if (GM == 1) fetch(g32 == 4 ? ib : ib * 4 / g32, s);   // on its way while the block is multiplied
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       uint32_t a[4], b[4];
@@ -161,27 +161,48 @@ struct Tile {
 };
 
 // ---- the router, in every cluster of CL blocks ----
-// part: [tokens][256] floats, partial logits by thread; logits: [tokens][experts]
-__device__ __forceinline__ void route(const Params& p, long long d_in, float* part, float* logits, Lists& L, int rank) {
+// part: [tokens][256] floats, partial logits by thread; logits: [tokens][experts]; xs: [8][512]
+__device__ __forceinline__ void route(const Params& p, long long d_in, float* part, float* logits, float* xs, Lists& L, int rank) {
   const int E = p.experts, T = p.tokens, k = p.top_k, tid = threadIdx.x;
   int ep = 8;
   while (ep < E) ep *= 2;
-  const int e = tid & (ep - 1), rg = tid / ep, groups = 256 / ep;
-  const long long i0 = d_in * rank / CL, i1 = d_in * (rank + 1) / CL;
+  const int e = tid & (ep - 1), rg = tid / ep, groups = 256 / ep, d = (int)d_in;
+  // this block's inputs, a multiple of four but for the last's; staged in fp32, 8 tokens x SUB inputs at a time (a thread that read X for itself took
+  // 100 instructions per input, and the router three times as long as the experts)
+  constexpr int SUB = 512;
+  const int i0 = min(d, (d + 4 * CL - 1) / (4 * CL) * 4 * rank), i1 = min(d, (d + 4 * CL - 1) / (4 * CL) * 4 * (rank + 1));
   for (int t0 = 0; t0 < T; t0 += 8) {
+    const int nt = min(8, T - t0);
     float acc[8] = {};
-    if (e < E) {
-#pragma unroll 4
-      for (long long i = i0 + rg; i < i1; i += groups) {
-        const float r = load_x(p.R, p.rt, i * E + e);
+    for (int s0 = i0; s0 < i1; s0 += SUB) {
+      const int len = min(SUB, i1 - s0);
+      __syncthreads();
+      for (int v = tid; v < nt * SUB; v += 256) {
+        const int t = v / SUB, i = v % SUB;
+        xs[v] = i < len ? load_x(p.X, p.xt, (t0 + t) * p.ldx + s0 + i) : 0.f;
+      }
+      __syncthreads();
+      if (e < E) {
+        auto steps = [&](auto get) {
+          for (int i = 4 * rg; i < len; i += 4 * groups) {
+            float r[4];
 #pragma unroll
-        for (int t = 0; t < 8; ++t)
-          if (t0 + t < T) acc[t] = fmaf(load_x(p.X, p.xt, (t0 + t) * p.ldx + i), r, acc[t]);
+            for (int u = 0; u < 4; ++u) r[u] = get((s0 + min(i + u, len - 1)) * E + e);   // (past the end X is zero)
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+              if (t < nt) {
+                const float4 x = *reinterpret_cast<const float4*>(xs + t * SUB + i);
+                acc[t] = fmaf(x.x, r[0], fmaf(x.y, r[1], fmaf(x.z, r[2], fmaf(x.w, r[3], acc[t]))));
+              }
+          }
+        };
+        if (p.rt == CDQ_BF16) steps([&](int at) { return __bfloat162float(((const __nv_bfloat16*)p.R)[at]); });
+        else steps([&](int at) { return ((const float*)p.R)[at]; });
       }
     }
 #pragma unroll
     for (int t = 0; t < 8; ++t)
-      if (t0 + t < T) part[(t0 + t) * 256 + tid] = acc[t];
+      if (t < nt) part[(t0 + t) * 256 + tid] = acc[t];
   }
   __syncthreads();
   for (int v = tid; v < T * E; v += 256) {   // this block's share of the inputs
@@ -286,7 +307,7 @@ __global__ void __launch_bounds__(256, 2) moe_up_kernel(const __grid_constant__ 
     mbar_fence_init();
   }
   __syncwarp();
-  route(p, p.gate.d_in, red, red + p.tokens * 256, L, blockIdx.x % CL);
+  route(p, p.gate.d_in, red + 4096, red + 4096 + p.tokens * 256, red, L, blockIdx.x % CL);
   __syncthreads();
   if (blockIdx.x == 0)
     for (int v = threadIdx.x; v < (int)(sizeof(Lists) / 4); v += 256) reinterpret_cast<int*>(p.lists)[v] = reinterpret_cast<const int*>(&L)[v];
@@ -469,7 +490,7 @@ template <int CW, int NT, int GM, bool F32>
 cudaError_t run(const Params& p, int sms, cudaStream_t st) {
   constexpr size_t ring = WARPS * kStages * (kChunk<CW> * Piece<CW>::BLOCK + 8), lists = (sizeof(Lists) + 15) / 16 * 16;
   constexpr size_t red = 2 * WARPS * 2 * 16 * NT * 8 * sizeof(float);
-  const size_t logits = (size_t)p.tokens * (256 + p.experts) * sizeof(float), router = logits > red ? logits : red;
+  const size_t logits = (4096 + (size_t)p.tokens * (256 + p.experts)) * sizeof(float), router = logits > red ? logits : red;
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute at[1];
   const long long most = (long long)p.gate.njt * (p.experts < p.tokens * p.top_k ? p.experts : p.tokens * p.top_k);
