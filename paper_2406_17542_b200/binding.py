@@ -594,7 +594,7 @@ def status_is_workspace(st: int) -> bool:
 
 def quantize_layer(X: torch.Tensor, W: torch.Tensor, grid: Grid, passes: int, lambda_rel: float = 0.0, mode="fast",
                    device="cuda:0", ws: Workspace | None = None, return_host: bool | None = None,
-                   init: str = "rtn", steps_per_col: int | None = None, bcd_steps: int = 0, seed: int = 0) -> dict:
+                   init: str = "rtn", steps_per_col: int | None = None, bcd_steps: int = 0, seed: int = 0, pack: bool = False) -> dict:
     """The whole hot path for one layer: Hessian, grid/codes, greedy CD, loss.
 
     X and W may live on the host (pinned memory makes the copies asynchronous): they are then
@@ -604,7 +604,8 @@ def quantize_layer(X: torch.Tensor, W: torch.Tensor, grid: Grid, passes: int, la
     The paper's variants around the main loop: init="owc_cd" takes the grid from cdq_init_owc_cd
     (per-group clipping strengths, needs grid.n_clip > 1) instead of cdq_init_rtn; steps_per_col
     gives the descent's budget in steps per column instead of passes * d_in; bcd_steps > 0 runs
-    that many steps of block coordinate descent with random pairs from the greedy solution."""
+    that many steps of block coordinate descent with random pairs from the greedy solution.
+    pack: "packed" is the solved layer as cdq_linear takes it, on the device."""
     if init not in ("rtn", "owc_cd"):
         raise ValueError("init must be 'rtn' or 'owc_cd'")
     on_host = not X.is_cuda
@@ -626,6 +627,8 @@ def quantize_layer(X: torch.Tensor, W: torch.Tensor, grid: Grid, passes: int, la
     else:   # the descent hands back the loss of its result
         stats, loss = cdq_cd_solve_with_loss(H, Wd, grid, scale, zero, Q, budget, mode=mode, ws=ws)
         out = {"H": H, "scale": scale, "zero": zero, "Q": Q, "gamma": gamma, "stats": stats, "loss": loss}
+    if pack:
+        out["packed"] = cdq_pack(Q, grid, scale, zero)
     if return_host:
         for k in ("scale", "zero", "Q"):
             out[k] = out[k].to("cpu", non_blocking=False)

@@ -27,7 +27,7 @@ PackedView view_of(const cdq_packed_layer& l) {
   v.z = 1 << (l.bits - 1);
   const int cw = packed_width(l.bits);
   for (int k = 0; k < 3; ++k) {   // places 0, CW and 2 CW within the seven bits; eight bits: -256
-    const float m = l.bits == 8 ? -256.f : -(ldexpf(128.f, -k * cw) + (float)v.z);
+    const float m = kDown * (l.bits == 8 ? -256.f : -(ldexpf(128.f, -k * cw) + (float)v.z));
     uint32_t b;
     memcpy(&b, &m, 4);
     v.minus[k] = (b >> 16) | (b & 0xffff0000u);

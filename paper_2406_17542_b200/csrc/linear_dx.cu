@@ -2,7 +2,7 @@
 //
 //   D[i, n] = sum_j W_hat[i, j] dZ[n, j],   W_hat[i, j] = a_t(i),j Q[i, j] + b_t(i),j
 //
-// The scales run along the sum, so they cannot wait for it: W_hat is formed in fp32 and rounded to bf16 for the tensor core (2^-9 of a weight, half a
+// The scales run along the sum, so they cannot wait for it: W_hat is formed in fp32 and rounded to bf16 for the tensor core (up to 2^-8 of a weight, half a
 // step of bf16, as any bf16 product of the layer would take it); so is dZ, unless it is dY itself.  fp32: both as three bf16 terms, the six products
 // that reach 2^-24.
 //
@@ -188,11 +188,11 @@ __global__ void __launch_bounds__(THREADS, 1) linear_dx_kernel(const __grid_cons
           // columns past the layer's: dZ is zero there (outside the tensor map or its padding), W_hat finite
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            const float av = a[v][CHUNKS ? c : 0], bv = fmaf((float)w.z, av, b[v][CHUNKS ? c : 0]);
+            const float a0 = a[v][CHUNKS ? c : 0], bv = fmaf((float)w.z, a0, b[v][CHUNKS ? c : 0]), av = kUp * a0;
             uint32_t r[TERMS][4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-              const uint32_t pair = dequant_pair<CW>(now[v], 4 * c + x, codec);   // code - z, twice
+              const uint32_t pair = dequant_pair<CW>(now[v], 4 * c + x, codec);   // (code - z) kDown, twice
               const float lo = fmaf(av, __uint_as_float(pair << 16), bv), hi = fmaf(av, __uint_as_float(pair & 0xffff0000u), bv);
               if (TERMS == 1) {
                 const __nv_bfloat162 y = __floats2bfloat162_rn(lo, hi);

@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(256, 2) linear_skinny_kernel(const __grid_cons
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) acc[t][v] = fmaf(v < 2 ? s[0] : s[2], P[t][v], (v < 2 ? b0 : b1) * S[t][v & 1]);
+      for (int v = 0; v < 4; ++v) acc[t][v] = fmaf(kUp * (v < 2 ? s[0] : s[2]), P[t][v], (v < 2 ? b0 : b1) * S[t][v & 1]);
   }
   // sums of the warps that share columns, then of the cluster's blocks, both in ascending order of the inputs' share
   const int cl = p.wj_log2 + 4, cols = 1 << cl, outs = cols * p.n, T = blockDim.x;

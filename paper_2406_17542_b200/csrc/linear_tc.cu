@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
           b1 = __ldg(w.zero + (long long)wk.t * w.d_out + j);
         }
         const float4* Sg = reinterpret_cast<const float4*>(sring + ss * (2 * NH) + h * NH);
-        const unsigned long long a2 = pack2(a, a), b2 = ends ? pack2(fmaf(zf, a, b), fmaf(zf, a, b)) : 0ull;
+        const unsigned long long a2 = pack2(kUp * a, kUp * a), b2 = ends ? pack2(fmaf(zf, a, b), fmaf(zf, a, b)) : 0ull;
         unsigned long long s2 = 0ull, z2 = 0ull;
         ok = warp_wait(dfull(h), dph, abort_flag, SPIN) && (!ends || warp_wait(sfull(ss), sph, abort_flag, SPIN));
         if (!ok) break;
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
           if (++ss == S_STAGES) { ss = 0; sph ^= 1u; }
         }
         if (GRAD) {
-          ds += lo2(s2) + hi2(s2);
+          ds = fmaf(kUp, lo2(s2) + hi2(s2), ds);
           if (ends) {
             const long long slot = tok0 / NH;
             const float dz = lo2(z2) + hi2(z2);

@@ -84,7 +84,7 @@ template <int CW> struct Codec {
     asm volatile("mov.b32 %0, 0x43004300;" : "=r"(magic));
 #pragma unroll
     for (int v = 0; v < PLACES; ++v) {
-      const uint32_t M = CW == 8 ? 0x7fu : ((1u << CW) - 1) << (v * CW), S = 0x3f80u - ((uint32_t)(v * CW) << 7);   // 2^-(v CW)
+      const uint32_t M = CW == 8 ? 0x7fu : ((1u << CW) - 1) << (v * CW), S = 0x3f80u - ((uint32_t)(v * CW + 8) << 7);   // 2^-(v CW) kDown
       asm volatile("mov.b32 %0, %1;" : "=r"(mask[v]) : "r"(M | M << 16));
       asm volatile("mov.b32 %0, %1;" : "=r"(scale[v]) : "r"(S | S << 16));
       minus[v] = w.minus[v];
@@ -98,8 +98,11 @@ __device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t s
   return r;
 }
 
-// code - z of pair p.  minus[v] = -(128 2^-(v CW) + z) twice; with eight bits -256, and the codes' top bits, put aside, make it -128:
-// 128 + (code & 127) - 128 where the bit is set, - 256 where it is not, is code - 128.  Five to seven bits: -(128 + z), and no top bits.
+// (code - z) kDown of pair p: brought down to below 1, so that sums of products stay within fp32 wherever the sums of the inputs do (scales go up by
+// kUp = 1 / kDown where they meet the sums; both are exact).  minus[v] = -(128 2^-(v CW) + z) kDown twice; with eight bits -256 kDown, and the codes'
+// top bits, put aside, halve it: 128 + (code & 127) - 128 where the bit is set, - 256 where it is not, is code - 128.  Five to seven bits:
+// -(128 + z) kDown, and no top bits.
+constexpr float kDown = 1.f / 256, kUp = 256.f;
 template <int CW>
 __device__ __forceinline__ uint32_t dequant_pair(const uint32_t* w, int p, const Codec<CW>& k) {
   if (CW == 8) {

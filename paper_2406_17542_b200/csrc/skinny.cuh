@@ -65,13 +65,13 @@ __device__ __forceinline__ void fetch_sums(const float* sums, float (&S)[NT][4])
 // acc += a P + (b + z a) S for the group's scales and zeros of the lane's two columns.
 template <int NT>
 __device__ __forceinline__ void promote(const float (&s)[4], float z, const float (&S)[NT][4], const float (&P)[NT][4], float (&acc)[NT][4]) {
-  const float b0 = fmaf(z, s[0], s[1]), b1 = fmaf(z, s[2], s[3]);
+  const float b0 = fmaf(z, s[0], s[1]), b1 = fmaf(z, s[2], s[3]), a0 = kUp * s[0], a1 = kUp * s[2];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    acc[t][0] = fmaf(s[0], P[t][0], fmaf(b0, S[t][0], acc[t][0]));
-    acc[t][1] = fmaf(s[0], P[t][1], fmaf(b0, S[t][1], acc[t][1]));
-    acc[t][2] = fmaf(s[2], P[t][2], fmaf(b1, S[t][0], acc[t][2]));
-    acc[t][3] = fmaf(s[2], P[t][3], fmaf(b1, S[t][1], acc[t][3]));
+    acc[t][0] = fmaf(a0, P[t][0], fmaf(b0, S[t][0], acc[t][0]));
+    acc[t][1] = fmaf(a0, P[t][1], fmaf(b0, S[t][1], acc[t][1]));
+    acc[t][2] = fmaf(a1, P[t][2], fmaf(b1, S[t][0], acc[t][2]));
+    acc[t][3] = fmaf(a1, P[t][3], fmaf(b1, S[t][1], acc[t][3]));
   }
 }
 
