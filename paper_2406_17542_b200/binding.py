@@ -398,13 +398,17 @@ class PackedLayer:
         self.ref = ctypes.pointer(cdq_packed_layer(codes.data_ptr(), scale.data_ptr(), zero.data_ptr(), d_in, d_out, bits, group_size))
 
 
+# the handle of a GPU's current stream without a Stream object around it (1.1 us less per call, of 12)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _call(fn, where: str, index: int, args):
     """fn(*args, stream) on GPU `index` and its current stream."""
     if torch.cuda.current_device() == index:
-        status = fn(*args, torch.cuda.current_stream(index).cuda_stream)
+        status = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
-            status = fn(*args, torch.cuda.current_stream(index).cuda_stream)
+            status = fn(*args, _raw_stream(index))
     if status:
         _check(status, where)
 

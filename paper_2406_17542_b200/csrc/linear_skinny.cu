@@ -9,10 +9,6 @@
 // thread blocks shares a long column.  X is staged in shared memory, the codes come by bulk copies into a ring per warp.  The sums of warps and
 // blocks are added in a fixed order, through shared memory and the cluster's shared memory: no workspace, no atomics, one launch.
 #include <cooperative_groups.h>
-#ifdef CDQ_TUNE
-#include <stdio.h>
-#include <stdlib.h>
-#endif
 
 #include "async_copy.cuh"
 #include "linear.cuh"
@@ -294,11 +290,16 @@ cudaError_t launch_linear_skinny(const PackedView& w, int cw, const void* X, lon
   p.bulk = ep.xt == CDQ_BF16 && ldx % 8 == 0 && w.d_in % 8 == 0 && aligned16(X);
   p.status = device_status_word();
   if (!p.status) return cudaErrorInvalidSymbol;
-  int wj = 2;
-  p.wk = 4; p.ck = 1;
-#ifdef CDQ_TUNE
-  if (const char* e = getenv("CDQ_SKINNY")) sscanf(e, "%d,%d,%d", &wj, &p.wk, &p.ck);
-#endif
+  // About 2048 warps: the inputs of a tile are shared out among wk warps of a block (up to 4) and ck blocks of a cluster until there are that many or a warp
+  // has one block of inputs left; blocks of eight warps, of fewer where they would not reach all SMs.  us for wj, wk, ck: 2048 x 16384 (3 bits)
+  // 4,2,1 6.5, 8,1,1 6.8, 2,4,1 7.9, 2,2,2 10.1; 4096 x 4096 (2 bits, groups, 8 rows) 2,4,2 7.7, 2,2,4 7.8, 1,8,1 8.6, 4,2,1 12.3, 8,1,1 18.7;
+  // 18432 x 73728 (3 bits, groups) 8,1,1 165, 4,2,1 170, 2,2,1 194, 1,8,1 219; 256 x 256 1,4,1 2.9, 2,4,1 2.9, 8,1,1 3.4, clusters 4.
+  int split = 1;
+  while (split < 32 && w.njt * split < 2048 && 2 * split <= w.nib) split *= 2;
+  p.wk = split < 4 ? split : 4;
+  p.ck = split / p.wk;
+  int wj = 8 / p.wk;
+  while (wj > 1 && w.njt / wj * p.ck < 148) wj /= 2;
   switch (cw) {
     case 2: return run<2>(p, wj, st);
     case 3: return run<3>(p, wj, st);
