@@ -33,9 +33,12 @@ struct Params {
 constexpr unsigned kWaitCycles = 1u << 30;   // about half a second
 
 // GM: where a group can end -- 0 nowhere (one group), 1 at blocks of 128 inputs, 2 at chunks of 32.
-template <int CW, int NT, int TERMS, int GM>
+// ROWSUMS: S is summed once per thread block and slab (20 instructions per row and block of 128 inputs) instead of by every warp with its products (8 more
+// matrix instructions per block of codes): 18432 x 73728 in groups, one row, 195 -> 165 us; eight rows of 4096 x 4096 take longer.
+template <int CW, int NT, int TERMS, int GM, bool ROWSUMS>
 __global__ void __launch_bounds__(256, 2) linear_skinny_kernel(const __grid_constant__ Params p) {
   extern __shared__ __align__(128) unsigned char smem[];
+  constexpr bool SUMS = TERMS > 1 || ROWSUMS;
   constexpr int W = Piece<CW>::WORDS, BLOCK = Piece<CW>::BLOCK, C = Ring<CW>::C, STAGES = Ring<CW>::STAGES, BYTES = Ring<CW>::BYTES;
   const PackedView& w = p.w;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, WJ = 1 << p.wj_log2, wj = warp & (WJ - 1), wk = warp >> p.wj_log2;
@@ -117,6 +120,10 @@ __global__ void __launch_bounds__(256, 2) linear_skinny_kernel(const __grid_cons
       stage_rows<TERMS, GM == 2 ? 32 : 128>(xs, pitch, term_at, sums, NT * 8, p.X, p.ldx, w.d_in, p.n, (long long)s0 * 128, (s1 - s0) * 128);
       __syncthreads();
     }
+    if (ROWSUMS) {
+      sum_rows<GM == 2 ? 32 : 128>(xs, pitch, sums, NT * 8, p.n, s1 - s0);
+      __syncthreads();
+    }
     for (; k < chunks && ib0 + k * cb < s1; k += p.wk) {
       ok = mbar_wait_clock32(bars + 8 * stage, phase, ok ? kWaitCycles : 1u) && ok;
       float now[GM == 1 ? C : 1][4];
@@ -142,20 +149,20 @@ __global__ void __launch_bounds__(256, 2) linear_skinny_kernel(const __grid_cons
             if (chunk * 32 >= (int)w.d_in) break;
             float s[4];
             scales(group_of(chunk), s);
-            mma_chunk<CW, NT, TERMS, true>(cd, c, codec, xb + 32 * c, row_at, term_at, P, S);
-            fetch_sums<NT, TERMS>(sums + (at * 4 + c) * (NT * 8) + 2 * q, S);
+            mma_chunk<CW, NT, TERMS, true, SUMS>(cd, c, codec, xb + 32 * c, row_at, term_at, P, S);
+            fetch_sums<NT, SUMS>(sums + (at * 4 + c) * (NT * 8) + 2 * q, S);
             promote<NT>(s, zf, S, P, acc);
           }
           return;
         }
-        mma_chunk<CW, NT, TERMS, GM == 1>(cd, 0, codec, xb, row_at, term_at, P, S);
+        mma_chunk<CW, NT, TERMS, GM == 1, SUMS>(cd, 0, codec, xb, row_at, term_at, P, S);
 #pragma unroll
-        for (int c = 1; c < 4; ++c) mma_chunk<CW, NT, TERMS, false>(cd, c, codec, xb + 32 * c, row_at, term_at, P, S);
+        for (int c = 1; c < 4; ++c) mma_chunk<CW, NT, TERMS, false, SUMS>(cd, c, codec, xb + 32 * c, row_at, term_at, P, S);
         const float* here = sums + at * (NT * 8) + 2 * q;
         if (GM == 1) {
-          fetch_sums<NT, TERMS>(here, S);
+          fetch_sums<NT, SUMS>(here, S);
           promote<NT>(s1, zf, S, P, acc);
-        } else if (TERMS > 1) {
+        } else if (SUMS) {
 #pragma unroll
           for (int t = 0; t < NT; ++t) { S[t][0] += here[8 * t]; S[t][1] += here[8 * t + 1]; }
         }
@@ -223,9 +230,9 @@ __global__ void __launch_bounds__(256, 2) linear_skinny_kernel(const __grid_cons
   }
 }
 
-template <int CW, int NT, int TERMS, int GM>
+template <int CW, int NT, int TERMS, int GM, bool ROWSUMS = false>
 cudaError_t launch(const Params& p, int blocks, size_t bytes, cudaStream_t st) {
-  auto kern = linear_skinny_kernel<CW, NT, TERMS, GM>;
+  auto kern = linear_skinny_kernel<CW, NT, TERMS, GM, ROWSUMS>;
   if (bytes > 48 * 1024) {   // (asked for on every call: 0.3 us of the host's time, and the attribute belongs to the current device)
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != cudaSuccess) return e;
@@ -252,6 +259,11 @@ cudaError_t launch(const Params& p, int blocks, size_t bytes, cudaStream_t st) {
 
 template <int CW, int NT, int TERMS>
 cudaError_t launch_gm(const Params& p, int blocks, size_t bytes, cudaStream_t st) {
+  if constexpr (NT * TERMS == 1)
+    if (2 * p.n <= 1 << p.wj_log2) {
+      if (p.w.ng == 1) return launch<CW, 1, 1, 0, true>(p, blocks, bytes, st);
+      return p.w.g % 128 == 0 ? launch<CW, 1, 1, 1, true>(p, blocks, bytes, st) : launch<CW, 1, 1, 2, true>(p, blocks, bytes, st);
+    }
   if (p.w.ng == 1) return launch<CW, NT, TERMS, 0>(p, blocks, bytes, st);
   return p.w.g % 128 == 0 ? launch<CW, NT, TERMS, 1>(p, blocks, bytes, st) : launch<CW, NT, TERMS, 2>(p, blocks, bytes, st);
 }

@@ -26,10 +26,9 @@ template <int CW> struct Ring {
 };
 
 // P += codes of 32 inputs (chunk c of the block) x rows; FIRST: P = instead.  xs: row 0 of the staged rows at the chunk's first input; row_at: where
-// the lane's row of every tile of eight starts, plus 8 (lane % 4).  One term (bf16): S, the sums of the rows, comes from the same instruction with ones
-// on the left, and lies where P lies; that costs 8 more instructions per block of 2048 codes, while summing every row as it is staged costs each thread
-// block the whole of X (8 rows x 4096 inputs: 8 us against 1).
-template <int CW, int NT, int TERMS, bool FIRST>
+// the lane's row of every tile of eight starts, plus 8 (lane % 4).  S, the sums of the rows, comes from the same instruction with ones on the left, and
+// lies where P lies, unless SUMS says that they were summed when they were staged.
+template <int CW, int NT, int TERMS, bool FIRST, bool SUMS>
 __device__ __forceinline__ void mma_chunk(const uint32_t* w, int c, const Codec<CW>& k, const __nv_bfloat16* xs, const int (&row_at)[NT], int term_at,
                                           float (&P)[NT][4], float (&S)[NT][4]) {
   constexpr int W = Piece<CW>::WORDS;
@@ -44,19 +43,19 @@ __device__ __forceinline__ void mma_chunk(const uint32_t* w, int c, const Codec<
       const uint4 x = *reinterpret_cast<const uint4*>(xs + row_at[t] + m * term_at);
       if (FIRST && m == 0) mma_16816_new(P[t], a[0], b[0], a[1], b[1], x.x, x.y);
       else mma_16816(P[t], a[0], b[0], a[1], b[1], x.x, x.y);
-      if (TERMS == 1) {
-        if (FIRST) mma_16816_new(S[t], ONES, ONES, ONES, ONES, x.x, x.y);
+      if (!SUMS) {
+        if (FIRST && m == 0) mma_16816_new(S[t], ONES, ONES, ONES, ONES, x.x, x.y);
         else mma_16816(S[t], ONES, ONES, ONES, ONES, x.x, x.y);
       }
       mma_16816(P[t], a[2], b[2], a[3], b[3], x.z, x.w);
-      if (TERMS == 1) mma_16816(S[t], ONES, ONES, ONES, ONES, x.z, x.w);
+      if (!SUMS) mma_16816(S[t], ONES, ONES, ONES, ONES, x.z, x.w);
     }
 }
 
-// S of the lane's rows 2 q, 2 q + 1 of every tile of eight from where stage_rows left them (more terms than one).
-template <int NT, int TERMS>
+// S of the lane's rows 2 q, 2 q + 1 of every tile of eight from where they were summed.
+template <int NT, bool SUMS>
 __device__ __forceinline__ void fetch_sums(const float* sums, float (&S)[NT][4]) {
-  if (TERMS > 1) {
+  if (SUMS) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) { S[t][0] = sums[8 * t]; S[t][1] = sums[8 * t + 1]; }
   }
@@ -114,6 +113,20 @@ __device__ __forceinline__ void stage_rows(__nv_bfloat16* xs, int pitch, int ter
         for (int d = 1; d < UNIT / 8; d *= 2) s += __shfl_xor_sync(half, s, d);
         if (c % UNIT == 0) sums[c / UNIT * spitch + r] = s;
       }
+    }
+}
+
+// Sums of staged bf16 rows over every UNIT (32 or 128) of `units` x UNIT inputs: a warp per 128 inputs of a row.
+template <int UNIT>
+__device__ __forceinline__ void sum_rows(const __nv_bfloat16* xs, int pitch, float* sums, int spitch, int rows, int blocks) {
+  const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  for (int r = 0; r < rows; ++r)
+    for (int b = threadIdx.x >> 5; b < blocks; b += warps) {
+      const uint2 v = *reinterpret_cast<const uint2*>(xs + r * pitch + b * 128 + lane * 4);
+      float s = (__uint_as_float(v.x << 16) + __uint_as_float(v.x & 0xffff0000u)) + (__uint_as_float(v.y << 16) + __uint_as_float(v.y & 0xffff0000u));
+#pragma unroll
+      for (int d = 1; d < UNIT / 4; d *= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
+      if (lane % (UNIT / 4) == 0) sums[(b * (128 / UNIT) + lane / (UNIT / 4)) * spitch + r] = s;
     }
 }
 
