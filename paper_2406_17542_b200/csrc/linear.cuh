@@ -13,7 +13,8 @@ cudaError_t launch_unpack(const void* packed, long long layers, long long d_in, 
 struct GradIn {
   const void* dY; const void* X; const void* Z;
   long long lddy, ldx, ldz, n;
-  cdq_dtype xt;
+  cdq_dtype xt;   // of X, Z and dX ...
+  cdq_dtype yt;   // ... and of dY: fp32 where it is dZ that dz32 left
   int act;
 };
 
@@ -31,6 +32,7 @@ cudaError_t launch_linear_tc(const PackedView& w, int cw, const void* X, cdq_dty
 cudaError_t launch_scale_grad_tc(const PackedView& w, int cw, const GradIn& in, float* dscale, float* dzero, void* ws, cudaStream_t st);
 
 // linear_dx.cu: the same layers
+cudaError_t launch_dz32(const GradIn& in, long long d_out, float* dz, cudaStream_t st);   // dZ = dY act'(Z) in fp32, [n][d_out]
 bool dx_tc_takes(const PackedView& w);
 size_t dx_tc_workspace(const PackedView& w, cdq_dtype xt, long long n);
 cudaError_t launch_dx_tc(const PackedView& w, int cw, const GradIn& in, void* dX, long long lddx, void* ws, cudaStream_t st);

@@ -109,8 +109,8 @@ size_t cdq_linear_backward_workspace_bytes(const cdq_packed_layer* layer, cdq_dt
   if (check_packed(layer) != CDQ_OK || !valid_type(xt) || n < 1 || n > kMaxRows) return 0;
   const PackedView w = view_of(*layer);
   if (!linear_tc_takes(w)) return 0;
-  const size_t a = linear_tc_workspace(w, xt, n, true), b = dx_tc_workspace(w, xt, n);   // one after the other in the same place
-  return a > b ? a : b;
+  const size_t a = linear_tc_workspace(w, xt, n, true), b = dx_tc_workspace(w, xt, n);
+  return align_up(sizeof(float) * n * w.d_out) + (a > b ? a : b);   // dZ in fp32 (activations), then one after the other in the same place
 }
 
 cdq_status cdq_linear_backward(const cdq_packed_layer* layer, const void* dY, cdq_dtype xt, long long n, long long lddy, const void* X, long long ldx,
@@ -127,9 +127,17 @@ cdq_status cdq_linear_backward(const cdq_packed_layer* layer, const void* dY, cd
   const PackedView w = view_of(*layer);
   const int cw = packed_width(layer->bits);
   GradIn in{};
-  in.dY = dY; in.X = X; in.Z = act == CDQ_ACT_NONE ? nullptr : Z; in.lddy = lddy; in.ldx = ldx; in.ldz = ldz; in.n = n; in.xt = xt; in.act = act;
+  in.dY = dY; in.X = X; in.Z = act == CDQ_ACT_NONE ? nullptr : Z; in.lddy = lddy; in.ldx = ldx; in.ldz = ldz; in.n = n; in.xt = in.yt = xt; in.act = act;
   cudaStream_t st = (cudaStream_t)stream;
   if (!workspace_ok(ws, ws_bytes, cdq_linear_backward_workspace_bytes(layer, xt, n))) return CDQ_ERR_WORKSPACE;
+  if (linear_tc_takes(w)) {
+    if (in.Z) {
+      float* dz = (float*)ws;
+      CDQ_CUDA(launch_dz32(in, w.d_out, dz, st));
+      in.dY = dz; in.lddy = w.d_out; in.yt = CDQ_F32; in.Z = nullptr;
+    }
+    ws = (char*)ws + align_up(sizeof(float) * n * w.d_out);
+  }
   if (dbias) CDQ_CUDA(launch_bias_grad(in, w.d_out, dbias, st));
   if (dscale || dzero) {
     if (linear_tc_takes(w)) CDQ_CUDA(launch_scale_grad_tc(w, cw, in, dscale, dzero, ws, st));

@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(256) dz_kernel(GradIn in, long long d_out, lon
   for (int e = 0; e < 8; ++e) {
     float d = 0.f;
     if (c + e < d_out) {
-      d = load_x(in.dY, in.xt, row * in.lddy + c + e);
+      d = load_x(in.dY, in.yt, row * in.lddy + c + e);
       if (in.Z) d *= act_slope(load_x(in.Z, in.xt, row * in.ldz + c + e), in.act);
     }
     x[e] = d;
@@ -313,6 +313,15 @@ __global__ void __launch_bounds__(256) dz_kernel(GradIn in, long long d_out, lon
   }
 #pragma unroll
   for (int m = 0; m < TERMS; ++m) *reinterpret_cast<uint4*>(out + (m * in.n + row) * kp + c) = make_uint4(r[m][0], r[m][1], r[m][2], r[m][3]);
+}
+
+// dZ = dY act'(Z) in fp32: every gradient starts from it (evaluated in the scales' kernel, once per group of columns and row, the slopes alone were 15000
+// instructions that sixteen warps fetched for every tile: 1021 x 2048 x 16384 took 543 us).
+__global__ void __launch_bounds__(256) dz32_kernel(GradIn in, long long d_out, float* __restrict__ dz) {
+  const long long c = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (c >= d_out) return;
+  for (long long r = blockIdx.y; r < in.n; r += gridDim.y)
+    dz[r * d_out + c] = load_x(in.dY, in.yt, r * in.lddy + c) * act_slope(load_x(in.Z, in.xt, r * in.ldz + c), in.act);
 }
 
 int rows_half(long long n, bool f32) { return n <= 32 ? 16 : n <= 64 ? 32 : n <= 128 || f32 ? 64 : 128; }
@@ -352,6 +361,12 @@ cudaError_t launch_nh(const CUtensorMap& map, const Params& p, int nh, bool f32,
 
 }  // namespace
 
+cudaError_t launch_dz32(const GradIn& in, long long d_out, float* dz, cudaStream_t st) {
+  const dim3 grid((unsigned)((d_out + 255) / 256), (unsigned)(in.n < 4096 ? in.n : 4096));
+  { dz32_kernel<<<grid, 256, 0, st>>>(in, d_out, dz); count_launch(); }
+  return cudaGetLastError();
+}
+
 bool dx_tc_takes(const PackedView& w) { return w.ng == 1 || w.g % 32 == 0; }
 
 size_t dx_tc_workspace(const PackedView& w, cdq_dtype xt, long long n) {
@@ -359,7 +374,7 @@ size_t dx_tc_workspace(const PackedView& w, cdq_dtype xt, long long n) {
 }
 
 cudaError_t launch_dx_tc(const PackedView& w, int cw, const GradIn& in, void* dX, long long lddx, void* ws, cudaStream_t st) {
-  const bool f32 = in.xt == CDQ_F32, direct = !f32 && !in.Z && in.lddy % 8 == 0 && aligned16(in.dY);
+  const bool f32 = in.xt == CDQ_F32, direct = in.yt == CDQ_BF16 && !in.Z && in.lddy % 8 == 0 && aligned16(in.dY);
   const int nh = rows_half(in.n, f32);
   Params p{};
   p.w = w; p.n = in.n;
@@ -384,9 +399,8 @@ cudaError_t launch_dx_tc(const PackedView& w, int cw, const GradIn& in, void* dX
       GradIn part = in;
       part.n = in.n;
       const long long rows = in.n - r0 < 65535 ? in.n - r0 : 65535;
-      const size_t es = f32 ? 4 : 2;
-      part.dY = (const char*)in.dY + r0 * in.lddy * es;
-      part.Z = in.Z ? (const char*)in.Z + r0 * in.ldz * es : nullptr;
+      part.dY = (const char*)in.dY + r0 * in.lddy * (in.yt == CDQ_F32 ? 4 : 2);
+      part.Z = in.Z ? (const char*)in.Z + r0 * in.ldz * (f32 ? 4 : 2) : nullptr;
       const dim3 grid((unsigned)((kp / 8 + 255) / 256), (unsigned)rows);
       if (f32) dz_kernel<3><<<grid, 256, 0, st>>>(part, w.d_out, kp, dz + r0 * kp);
       else dz_kernel<1><<<grid, 256, 0, st>>>(part, w.d_out, kp, dz + r0 * kp);

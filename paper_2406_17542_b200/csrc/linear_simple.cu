@@ -135,15 +135,23 @@ __global__ void __launch_bounds__(256) scale_grad_simple_kernel(PackedView w, in
 }
 
 // dbias[j] = sum_n dZ[n, j]: 32 columns per block, 32 rows at a time, then the 32 partial sums in ascending order.
-__global__ void __launch_bounds__(1024) bias_grad_kernel(const void* __restrict__ dY, cdq_dtype xt, long long n, long long d_out, long long lddy,
+__global__ void __launch_bounds__(1024) bias_grad_kernel(const void* __restrict__ dY, cdq_dtype yt, cdq_dtype xt, long long n, long long d_out, long long lddy,
                                                          const void* __restrict__ Zin, long long ldz, int act, float* __restrict__ dbias) {
   __shared__ float part[32][33];
   const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
   const long long j = (long long)blockIdx.x * 32 + c;
   float s = 0.f;
-  if (j < d_out)
+  if (j < d_out && !Zin) {
+    if (yt == CDQ_BF16) {
+#pragma unroll 8
+      for (long long k = r; k < n; k += 32) s += __bfloat162float(((const __nv_bfloat16*)dY)[k * lddy + j]);
+    } else {
+#pragma unroll 8
+      for (long long k = r; k < n; k += 32) s += ((const float*)dY)[k * lddy + j];
+    }
+  } else if (j < d_out)
     for (long long k = r; k < n; k += 32) {
-      float d = load_x(dY, xt, k * lddy + j);
+      float d = load_x(dY, yt, k * lddy + j);
       if (Zin) d *= act_slope(load_x(Zin, xt, k * ldz + j), act);
       s += d;
     }
@@ -177,7 +185,7 @@ cudaError_t launch_scale_grad_simple(const PackedView& w, int cw, const GradIn& 
 }
 
 cudaError_t launch_bias_grad(const GradIn& in, long long d_out, float* dbias, cudaStream_t st) {
-  { bias_grad_kernel<<<(unsigned)((d_out + 31) / 32), 1024, 0, st>>>(in.dY, in.xt, in.n, d_out, in.lddy, in.Z, in.ldz, in.act, dbias); count_launch(); }
+  { bias_grad_kernel<<<(unsigned)((d_out + 31) / 32), 1024, 0, st>>>(in.dY, in.yt, in.xt, in.n, d_out, in.lddy, in.Z, in.ldz, in.act, dbias); count_launch(); }
   return cudaGetLastError();
 }
 

@@ -312,21 +312,16 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
       const int jb = t % p.jtiles * BJ + quarter * 32;
       const long long j = min((long long)jb + lane, w.d_out - 1), tok0 = (long long)(t / p.jtiles) * (2 * NH) + h * NH;
       if (GRAD) {
+        // dZ of the thread's column: rows past n repeat the last one's address and count as zero, so that the loads need not wait for one another
+        auto fill = [&](auto get) {
 #pragma unroll
-        for (int i = 0; i < NH; i += 2) {
-          float v[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const long long tok = tok0 + i + e;
-            float d = 0.f;
-            if (tok < p.n) {
-              d = load_x(p.in.dY, p.in.xt, tok * p.in.lddy + j);
-              if (p.in.Z) d *= act_slope(load_x(p.in.Z, p.in.xt, tok * p.in.ldz + j), p.in.act);
-            }
-            v[e] = d;
+          for (int i = 0; i < NH; i += 2) {
+            const float a = get(min(tok0 + i, p.n - 1) * p.in.lddy + j), b = get(min(tok0 + i + 1, p.n - 1) * p.in.lddy + j);
+            acc[i / 2] = pack2(tok0 + i < p.n ? a : 0.f, tok0 + i + 1 < p.n ? b : 0.f);
           }
-          acc[i / 2] = pack2(v[0], v[1]);
-        }
+        };
+        if (p.in.yt == CDQ_BF16) fill([&](long long at) { return __bfloat162float(((const __nv_bfloat16*)p.in.dY)[at]); });
+        else fill([&](long long at) { return ((const float*)p.in.dY)[at]; });
       } else {
 #pragma unroll
         for (int i = 0; i < NH / 2; ++i) acc[i] = 0ull;
