@@ -13,10 +13,15 @@
 //     loads a few blocks ahead, made into bf16 by four warps, lane = column, and stored into TMEM, where the tensor core takes its left
 //     operand from: shared memory carries X alone;
 //   * per block the first accumulator's instructions, then the second's: while one is multiplied into, the other's group goes through the scales;
-//   * warp 0 TMA, warp 1 MMA and TMEM owner, warps 4-7 codes, warps 8-11 and 12-15 the two accumulators: acc = fma(a, D, fma(b', S, acc)) in packed fp32;
+//   * warp 0 TMA, warp 1 MMA and TMEM owner, warp 2 the rows' sums, warps 4-7 codes, warps 8-11 and 12-15 the two accumulators:
+//     acc = fma(a, D, fma(b', S, acc)) in packed fp32;
 //   * persistent blocks over the tiles; few tiles: a cluster of CK blocks shares the inputs of one and adds its sums over the cluster's shared memory.
 // A long group is cut (flush_blocks).
 // Every wait is bounded, see async_copy.cuh.
+//
+// Measured: 8192 x 2048 x 16384 per channel with GELU 593 us = 0.93 PFLOP/s (bound by the epilogue, 27 K cycles per tile against 17 K of products);
+// 2048 x 4096 x 4096 in groups of 128 160 us (bound by the scales: 2150 cycles per group and tile against 1050); 61 x 14336 x 4096 33 us.
+// Tiles of 256 rows: codes are made once for 256 rows (450 cycles per block) and the instructions of both halves take 1050.
 #include <cuda.h>
 
 #include "async_copy.cuh"

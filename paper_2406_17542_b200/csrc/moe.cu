@@ -10,6 +10,9 @@
 // Bound by the bytes of the chosen experts.  A warp's codes come by bulk copies into a ring of its own that runs on across tiles, matrices and experts; the
 // rows come from L1.  The router is computed by every cluster of four blocks for itself (each a quarter of the inputs, exchanged over the
 // cluster's shared memory), which costs a microsecond and saves a launch and a pass over memory.  Everything is added in a fixed order.
+// Measured: one token, two of eight experts of 4096 x 14336, 4 bits: 176 us = 1.0 TB/s; five tokens, eight of 64 experts of 2048 x 1024, 3 bits in groups of
+// 128: 171 us (131 and 50 for the two kernels, 36 and 15 million warp instructions, of which the products are 16 and 10): bound by the instructions
+// and latencies around stretches of two to four blocks per warp, matrix and tile.
 #include "async_copy.cuh"
 #include "linear.cuh"
 #include "skinny.cuh"
@@ -90,10 +93,12 @@ template <int CW, int NT, int TERMS, int GM, bool F32>
 struct Tile {
   float acc[NT][4], P[NT][4], S[NT][4];
   const float *scale, *zero;
-  int dj, g32, d_in;
+  int dj, g32, d_in, last;
   float z;
   long long d_out;
-  __device__ __forceinline__ void start(const PackedView& w, int jt) {
+  float sc[4];   // GM 0, 1: scales and zeros of the group at hand, asked for a block ahead
+  __device__ __forceinline__ int group(int ib) const { return g32 == 4 ? ib : ib * 4 / g32; }
+  __device__ __forceinline__ void start(const PackedView& w, int jt, int ib) {   // ib: the stretch's first block
     const int row = (threadIdx.x & 31) >> 2;
     const long long j0 = min((long long)jt * 16 + row, w.d_out - 1), j1 = min((long long)jt * 16 + row + 8, w.d_out - 1);
     scale = w.scale + j0; zero = w.zero + j0; dj = (int)(j1 - j0);
@@ -102,6 +107,8 @@ struct Tile {
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int v = 0; v < 4; ++v) acc[t][v] = P[t][v] = S[t][v] = 0.f;
+    if (GM < 2) fetch(GM == 0 ? 0 : min(group(ib), w.ng - 1), sc);
+    last = w.ng - 1;
   }
   __device__ __forceinline__ void fetch(int group, float (&s)[4]) const {
     const long long at = group * d_out;
@@ -126,7 +133,11 @@ struct Tile {
     load_piece<CW>(codes, Piece<CW>::part(row, q), w);
     load_piece<CW>(codes, Piece<CW>::part(row + 8, q), w + W);
     float s[4];
-    if (GM == 1) fetch(g32 == 4 ? ib : ib * 4 / g32, s);   // on its way while the block is multiplied
+    if (GM == 1) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) s[v] = sc[v];
+      fetch(min(group(ib + 1), last), sc);
+    }
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       uint32_t a[4], b[4];
@@ -156,7 +167,7 @@ struct Tile {
     }
   }
   __device__ __forceinline__ void finish() {
-    if (GM == 0) scales(0);
+    if (GM == 0) promote<NT>(sc, z, S, P, acc);
   }
 };
 
@@ -344,7 +355,7 @@ __global__ void __launch_bounds__(256, 2) moe_up_kernel(const __grid_constant__ 
     float* out = red + ((parity * WARPS + warp) * 2) * (16 * NT * 8);
 #pragma unroll 1
     for (int m = 0; m < 2; ++m) {
-      tile.start(expert_view(m ? p.up : p.gate, p.codes_ff, e), jt);
+      tile.start(expert_view(m ? p.up : p.gate, p.codes_ff, e), jt, b0);
       for (int c = 0; c < cpm; ++c) {
         ok = mbar_wait_clock32(bars + 8 * stage, phase, ok ? kWait : 1u) && ok;
         const int first = b0 + c * C, have = min(C, b1 - first);
@@ -425,7 +436,7 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const __grid_constant_
     int rows[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) rows[t] = L.pair[s0 + min(t * 8 + row, n - 1)];
-    tile.start(expert_view(p.down, p.codes_dm, L.expert[a]), jt);
+    tile.start(expert_view(p.down, p.codes_dm, L.expert[a]), jt, f - a * nib);
     while (f < fe) {
       const int have = chunk(f);
       ok = mbar_wait_clock32(bars + 8 * stage, phase, ok ? kWait : 1u) && ok;

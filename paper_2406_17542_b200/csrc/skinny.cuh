@@ -18,8 +18,8 @@ __device__ __forceinline__ void mma_16816_new(float (&d)[4], uint32_t a0, uint32
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
-// A warp's codes come by bulk copies into a ring of its own: C blocks (2 KB and a little) per copy, STAGES copies in flight, so that an SM with 16 warps
-// has 128 KB on the way.  (Loads into registers five blocks ahead, the first version, left the warps waiting for memory half the time: 18432 x 16384,
+// A warp's codes come by bulk copies into a ring of its own: C blocks (2 to 3 KB) per copy, STAGES copies, so that an SM with 16 warps has 48 to 96 KB on
+// the way; 44 KB cover a microsecond of DRAM.  (Loads into registers five blocks ahead, the first version, left the warps waiting for memory half the time: 18432 x 16384,
 // 3 bits, 76 us.)
 template <int CW> struct Ring {
   static constexpr int C = CW == 2 ? 6 : CW == 3 ? 4 : CW == 4 ? 3 : 1, STAGES = 2, BYTES = C * Piece<CW>::BLOCK;
